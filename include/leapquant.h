@@ -80,6 +80,9 @@ extern "C" {
 /* bits of the sticky device error word */
 #define LQ_DEVERR_WINDOW_FULL 1   /* decode_step on a tile with rec_len == window      */
 #define LQ_DEVERR_BAD_REC_LEN 2   /* a tile's rec_len is outside [0, window]; untouched */
+#define LQ_DEVERR_BAD_SEQLENS 4   /* cu_seqlens falls, or leaves [0, tokens]             */
+#define LQ_DEVERR_BAD_SLOT    8   /* a slot >= n_slots                                   */
+#define LQ_DEVERR_BAD_POSITION 16 /* a position outside [0, n_positions)                 */
 
 /* Limits of this version. */
 #define LQ_MAX_COMP        16
@@ -283,6 +286,164 @@ int32_t leapquant_dequantize_state(const lq_dims *dims, const lq_state *st, floa
  * LQ_OK otherwise (LQ_EHIP if synchronisation failed).
  */
 int32_t leapquant_check_error(const lq_state *st, void *stream, int32_t *bits_out);
+
+/*
+ * ---- layer operators around the decode step -------------------------------
+ *
+ * What a layer runs before and beside the recurrent state: the short causal
+ * convolution of its channels, the norm and the position rotation of its
+ * queries and keys, and the selective state space scan, for whole prompts
+ * (packed sequences) and for single tokens.  The final state of a prompt's
+ * scan is in the layout that leapquant_quantize_state takes.
+ *
+ * Conventions beside those above:
+ *  - A token array has a row per token, `*_stride` elements apart; within a row
+ *    it is dense.  Rows start at multiples of 16 bytes (pointer and stride;
+ *    dt: of its element), so a slice of a projection's output can be passed.
+ *  - Tokens are fp32 or bf16 (LQ_TOKEN_*); parameters (weights, biases, A, skip,
+ *    cos, sin) are fp32, dense.  Arithmetic is fp32 or wider whatever the
+ *    tokens' type; outputs are rounded once, to nearest even.
+ *  - Packed sequences: sequence b holds the tokens [cu_seqlens[b],
+ *    cu_seqlens[b+1]), int32 on the device; empty ones are allowed, and tokens
+ *    at or past the last entry belong to none (their output is not written).
+ *    Entries that fall or leave [0, tokens] raise LQ_DEVERR_BAD_SEQLENS; they
+ *    are clamped, and what is computed from them is unspecified.
+ *  - Slots: the state of sequence (request) b is row slots[b] of the state
+ *    array, or row b where slots is NULL (then n_slots >= sequences).  A
+ *    negative slot is no state: the sequence starts from zero and its state is
+ *    not kept (padding of a captured batch).  A slot >= n_slots raises
+ *    LQ_DEVERR_BAD_SLOT: the sequence starts from NaN and is not kept.  No two
+ *    sequences of a call may share a slot.
+ *  - States are updated in place; other outputs must not overlap an input
+ *    (leapquant_qk_norm's may be its inputs).  A token that is not finite
+ *    changes neither earlier tokens of its sequence nor other sequences.
+ *  - `err` (optional, NULL: none) is a sticky error word as lq_state.err; an
+ *    lq_state of which only err is set may be given to leapquant_check_error.
+ */
+#define LQ_TOKEN_F32  0
+#define LQ_TOKEN_BF16 1
+#define LQ_NORM_NONE  0      /* y = x                                                */
+#define LQ_NORM_L2    1      /* y = x / sqrt(sum x^2 + eps)                          */
+#define LQ_NORM_RMS   2      /* y = x / sqrt(mean x^2 + eps) (times the weight)      */
+#define LQ_MAX_CONV_WIDTH 4
+
+/*
+ * Short causal convolution per channel:
+ *   y[t][c] = act(bias[c] + sum_{i < width} weight[c][width-1-i] x[t-i][c])
+ * within a sequence; x before its start is the state's last rows (carry) or 0.
+ * act is silu(y) = y / (1 + exp(-y)) or the identity.  The state then holds
+ * the last width-1 inputs of the sequence, oldest first.
+ * channels must be a multiple of 8 (bf16) or 4 (fp32), width 2..4.
+ */
+typedef struct {
+    int32_t seqs;               /* sequences; the step: requests                    */
+    int32_t channels;
+    int32_t width;
+    int32_t dtype;              /* x and state: LQ_TOKEN_*                          */
+    int32_t out_dtype;          /* out                                              */
+    int32_t silu;               /* 1: silu, 0: identity                             */
+    int32_t carry;              /* prompt: 1: start from the state, 0: from zero    */
+    int32_t n_slots;            /* rows of state                                    */
+    int64_t tokens;             /* rows of x and out (the step: requests)           */
+    int64_t x_stride, out_stride;
+    const void *x;              /* [tokens][channels]                               */
+    const float *weight;        /* [channels][width]                                */
+    const float *bias;          /* [channels] or NULL                               */
+    void *out;                  /* [tokens][channels]                               */
+    void *state;                /* [n_slots][width-1][channels]; prompt: may be NULL
+                                 * without carry                                    */
+    const int32_t *cu_seqlens;  /* [seqs + 1] (the step does not read it)           */
+    const int32_t *slots;       /* [seqs] or NULL                                   */
+    int32_t *err;
+} lq_conv;
+
+/* leapquant_conv_prompt -- all tokens of packed sequences. */
+int32_t leapquant_conv_prompt(const lq_conv *c, void *stream);
+
+/* leapquant_conv_step -- one token of every request (row b of x), always from
+ * its state, which moves on by that token. */
+int32_t leapquant_conv_step(const lq_conv *c, void *stream);
+
+/*
+ * leapquant_qk_norm -- norm of every query and key head, then the rotation of
+ * its first `rot` channels by the token's position, in one pass:
+ *   (a, b) -> (a cos - b sin, b cos + a sin),  cos, sin = table[position][j]
+ * over the pairs (j, j + rot/2), or (2j, 2j+1) if interleaved; queries are then
+ * multiplied by q_scale.  d is 64, 128 or 256; rot a multiple of 16, 0: none.
+ * A position outside the table raises LQ_DEVERR_BAD_POSITION and gives NaN in
+ * the rotated channels.  q_out, k_out may be q, k (same type and stride).
+ */
+typedef struct {
+    int64_t tokens;
+    int32_t heads_q, heads_k;   /* heads_k may be 0: queries only                   */
+    int32_t d;
+    int32_t norm;               /* LQ_NORM_*                                        */
+    int32_t rot;
+    int32_t interleaved;
+    int32_t dtype, out_dtype;
+    float eps, q_scale;
+    int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+    const void *q, *k;          /* [tokens][heads][d]                               */
+    void *q_out, *k_out;
+    const float *q_weight, *k_weight;   /* [d] or NULL (ones); LQ_NORM_RMS only     */
+    const float *cos, *sin;     /* [n_positions][rot/2] (rot > 0)                   */
+    const int32_t *positions;   /* [tokens] (rot > 0)                               */
+    int32_t n_positions;
+    int32_t *err;
+} lq_qk;
+int32_t leapquant_qk_norm(const lq_qk *n, void *stream);
+
+/*
+ * Selective state space scan: with delta = softplus(dt + dt_bias) (or the sum
+ * itself) and alpha = exp(delta A), per value head (App. A, the b_t = 0 rows
+ * with a scalar gate; beta = delta in leapquant_decode_step's terms)
+ *   S_t = alpha_t S_{t-1} + delta_t k_t v_t^T,   o_t = S_t^T q_t + skip v_t.
+ * The shapes are dims': batch sequences, heads_v, heads_k, d_k = d_v = 128, the
+ * scalar gate and LQ_RULE_ADD (LQ_EUNSUPPORTED otherwise).
+ */
+typedef struct {
+    int64_t tokens;             /* rows of q, k, v, dt, o (the step: dims->batch)   */
+    int32_t dtype;              /* q, k, v, dt, o: LQ_TOKEN_*                       */
+    int32_t state_dtype;        /* LQ_STATE_F32; the step also LQ_STATE_BF16        */
+    int32_t softplus;           /* 1: delta = softplus(dt + bias), 0: dt + bias     */
+    int32_t carry;              /* prompt: 1: start from the state, 0: from zero    */
+    int32_t n_slots;            /* rows of state                                    */
+    int32_t max_len;            /* prompt: longest sequence if known, 0 if not.  A
+                                 * hint for how the work is split: results do not
+                                 * depend on it beyond the order of sums            */
+    int64_t q_stride, k_stride, v_stride, dt_stride, o_stride;
+    const void *q, *k;          /* [tokens][heads_k][d_k]                           */
+    const void *v;              /* [tokens][heads_v][d_v]                           */
+    const void *dt;             /* [tokens][heads_v]                                */
+    const float *A;             /* [heads_v], decay rates (negative)                */
+    const float *skip;          /* [heads_v] or NULL (0)                            */
+    const float *dt_bias;       /* [heads_v] or NULL (0)                            */
+    void *o;                    /* [tokens][heads_v][d_v]                           */
+    void *state;                /* [n_slots][heads_v][d_v][d_k], S^T; the prompt may
+                                 * pass NULL without carry                          */
+    const int32_t *cu_seqlens;  /* [batch + 1] (the step does not read it)          */
+    const int32_t *slots;       /* [batch] or NULL                                  */
+    int32_t *err;
+    void *workspace;            /* 16-byte aligned device memory, overwritten       */
+    size_t workspace_bytes;
+} lq_scan;
+
+/* leapquant_scan_workspace_bytes -- host only: workspace that
+ * leapquant_scan_prompt needs for these shapes, tokens and max_len (may be 0). */
+int32_t leapquant_scan_workspace_bytes(const lq_dims *dims, const lq_scan *s, size_t *bytes_out);
+
+/* leapquant_scan_prompt -- all tokens of packed sequences, fp32 states. */
+int32_t leapquant_scan_prompt(const lq_dims *dims, const lq_scan *s, void *stream);
+
+/* leapquant_scan_step -- one token of every request (row b of the token
+ * arrays), always from its dense state.  A bf16 state is rounded to nearest
+ * even after the update and the output reads the rounded state. */
+int32_t leapquant_scan_step(const lq_dims *dims, const lq_scan *s, void *stream);
+
+/* leapquant_scan_gates -- alpha = exp(delta A) and beta = delta, [tokens][heads_v]
+ * fp32 each, of the scan's dt: the gates that leapquant_decode_step takes under
+ * LQ_RULE_ADD.  Reads tokens, dtype, softplus, dt, dt_stride, A and dt_bias. */
+int32_t leapquant_scan_gates(const lq_dims *dims, const lq_scan *s, float *alpha, float *beta, void *stream);
 
 /* Static description of a status code. */
 const char *leapquant_strerror(int32_t status);

@@ -11,6 +11,8 @@ from .binding import (  # noqa: F401
     leapquant_window_commit,
     leapquant_baseline_step, leapquant_baseline_step_general, leapquant_dequantize_state,
     leapquant_check_error,
+    leapquant_conv_prompt, leapquant_conv_step, leapquant_qk_norm, leapquant_scan_prompt, leapquant_scan_step,
+    leapquant_scan_gates, leapquant_scan_workspace_bytes, leapquant_check_error_word,
 )
 
 __all__ = [
@@ -18,4 +20,6 @@ __all__ = [
     "leapquant_quantize_state", "leapquant_decode_step", "leapquant_decode_step_general",
     "leapquant_decode_step_commit", "leapquant_window_commit", "leapquant_baseline_step", "leapquant_baseline_step_general",
     "leapquant_dequantize_state", "leapquant_check_error",
+    "leapquant_conv_prompt", "leapquant_conv_step", "leapquant_qk_norm", "leapquant_scan_prompt",
+    "leapquant_scan_step", "leapquant_scan_gates", "leapquant_scan_workspace_bytes", "leapquant_check_error_word",
 ]

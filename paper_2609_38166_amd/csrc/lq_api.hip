@@ -12,19 +12,15 @@ namespace {
 
 thread_local char g_last_hip[256] = "";
 
+}  // namespace
+
+namespace lq {
+
 int32_t hip_status(hipError_t e) {
     if (e == hipSuccess) return LQ_OK;
     strncpy(g_last_hip, hipGetErrorString(e), sizeof(g_last_hip) - 1);
     g_last_hip[sizeof(g_last_hip) - 1] = '\0';
     return LQ_EHIP;
-}
-
-bool aligned(const void *p) { return ((uintptr_t)p & 15u) == 0; }
-
-int32_t check_ptr(const void *p) {
-    if (!p) return LQ_EINVAL;
-    if (!aligned(p)) return LQ_EALIGN;
-    return LQ_OK;
 }
 
 int32_t check_dims(const lq_dims *d) {
@@ -53,6 +49,21 @@ int32_t check_dims(const lq_dims *d) {
     const long long tiles = (long long)d->batch * d->heads_v;
     if (tiles > (1LL << 30)) return LQ_EUNSUPPORTED;
     if (tiles * (d->heads_v / d->heads_k) >= (1LL << 32)) return LQ_EUNSUPPORTED;
+    return LQ_OK;
+}
+
+}  // namespace lq
+
+namespace {
+
+using lq::check_dims;
+using lq::hip_status;
+
+bool aligned(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+int32_t check_ptr(const void *p) {
+    if (!p) return LQ_EINVAL;
+    if (!aligned(p)) return LQ_EALIGN;
     return LQ_OK;
 }
 
@@ -251,10 +262,10 @@ const char *leapquant_strerror(int32_t status) {
     switch (status) {
         case LQ_OK: return "success";
         case LQ_EINVAL: return "invalid argument (NULL pointer, non-positive size or bad enum)";
-        case LQ_EALIGN: return "pointer not aligned (16 bytes; 4 for beta, scalar-gate alpha, rec_len, err "
-                               "and mask; 2 for scalar-gate rec_a)";
+        case LQ_EALIGN: return "pointer or token stride not aligned (16 bytes; 4 for beta, scalar-gate alpha, rec_len, "
+                               "err, mask and the layer operators' per-head and index arrays; 2 for scalar-gate rec_a)";
         case LQ_EUNSUPPORTED: return "unsupported shape or parameter (d_k/d_v must be 128, r <= 16, "
-                                     "W within the gate's limit)";
+                                     "W within the gate's limit; the layer operators' limits are in leapquant.h)";
         case LQ_EHIP: return "HIP runtime error (see leapquant_last_hip_error)";
         case LQ_EDEVICE: return "device-side error flag was set (e.g. decode on a full window)";
         default: return "unknown status";

@@ -1,0 +1,268 @@
+// Short causal convolution per channel, prompts (packed sequences) and single
+// tokens:  y[t][c] = act(bias[c] + sum_i w[c][K-1-i] x[t-i][c]).
+//
+// Bound: HBM; K multiply-adds per value read.  A thread owns 16 bytes of
+// channels of a run of tokens, whose input rows it reads once into registers;
+// neighbouring lanes own neighbouring channels, so every access is whole lines.
+#include "lq_layer.hpp"
+#include "lq_internal.hpp"
+
+namespace lq {
+
+namespace {
+
+constexpr int RUN = 16;     // tokens of a wave
+
+struct ConvArgs {
+    const char *x;
+    const float *weight, *bias;
+    char *out;
+    char *state;
+    const int32_t *cu, *slots;
+    int32_t *err;
+    int64_t tokens, x_stride, out_stride;      // strides in bytes
+    int32_t seqs, channels, n_slots, silu, carry, blocks_c, blocks_t;
+};
+
+template <int K, bool BF>
+__device__ __forceinline__ void load_params(const ConvArgs &a, int c, float (*w)[K], float *bias) {
+    constexpr int V = Tok<BF>::V;
+    float flat[V * K];
+#pragma unroll
+    for (int i = 0; i < V * K / 4; ++i) {
+        const float4 p = ((const float4 *)(a.weight + (int64_t)c * K))[i];
+        flat[4 * i] = p.x; flat[4 * i + 1] = p.y; flat[4 * i + 2] = p.z; flat[4 * i + 3] = p.w;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+#pragma unroll
+        for (int j = 0; j < K; ++j) w[v][j] = flat[v * K + j];
+        bias[v] = a.bias ? a.bias[c + v] : 0.0f;
+    }
+}
+
+// Output of one token from its K input rows (oldest first).
+template <int K, bool BF, bool OBF>
+__device__ __forceinline__ void emit(const ConvArgs &a, char *to, const uint4 *rows, const float (*w)[K], const float *bias) {
+    constexpr int V = Tok<BF>::V;
+    float y[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) y[v] = bias[v];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        float f[V];
+        unpack16<BF>(rows[j], f);
+#pragma unroll
+        for (int v = 0; v < V; ++v) y[v] = fmaf(w[v][j], f[v], y[v]);
+    }
+    if (a.silu) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) y[v] *= __builtin_amdgcn_rcpf(1.0f + __expf(-y[v]));
+    }
+    store_tok<OBF, V>(to, y);
+}
+
+__device__ __forceinline__ uint4 fill16(uint32_t w) { return make_uint4(w, w, w, w); }
+
+// Row `i` (0 oldest) of what precedes a sequence: its state, zero, or NaN.
+template <int K, bool BF>
+__device__ __forceinline__ uint4 old_row(const ConvArgs &a, int slot, int i, int64_t c_bytes) {
+    if (slot == BAD_SLOT) return fill16(BF ? 0x7FC07FC0u : 0x7FC00000u);
+    if (!a.carry || slot == NO_SLOT) return fill16(0u);
+    return *(const uint4 *)(a.state + ((int64_t)slot * (K - 1) + i) * a.channels * Tok<BF>::BYTES + c_bytes);
+}
+
+// Last sequence that begins at or before token t (-1: none), over the seqs
+// entries of cu; the whole wave searches, 64 entries at a time.
+__device__ __forceinline__ int find_sequence(const int32_t *cu, int seqs, int64_t t, int lane) {
+    int lo = 0, hi = seqs;                       // the count of entries <= t lies in [lo, hi]
+    while (hi - lo > 64) {
+        const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const int p = __popcll(__ballot(at < hi && cu[at < hi ? at : lo] <= t));
+        if (p == 0) return lo - 1;
+        hi = min(hi, lo + p * step);
+        lo = lo + (p - 1) * step + 1;
+    }
+    const int at = lo + lane;
+    return lo + __popcll(__ballot(at < hi && cu[at < hi ? at : 0] <= t)) - 1;
+}
+
+// A token whose window reaches the sequence's start, from memory.
+template <int K, bool BF, bool OBF>
+__device__ __forceinline__ void emit_first(const ConvArgs &a, int64_t t, int64_t begin, int slot, int64_t c_bytes,
+                                        const float (*w)[K], const float *bias, int c) {
+    uint4 rows[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        const int64_t at = t - (K - 1) + j;
+        rows[j] = at >= begin ? *(const uint4 *)(a.x + at * a.x_stride + c_bytes)
+                              : old_row<K, BF>(a, slot, (int)(K - 1 + at - begin), c_bytes);
+    }
+    emit<K, BF, OBF>(a, a.out + t * a.out_stride + (int64_t)c * Tok<OBF>::BYTES, rows, w, bias);
+}
+
+// One wave: RUN tokens of 64 lanes' channels.  The first K-1 tokens of a
+// sequence read the old state and its last K-1 replace it in place, so the wave
+// that holds a sequence's first token computes all of those K-1 tokens (also
+// past its run) and then writes the new state: nobody else reads the old one.
+template <int K, bool BF, bool OBF>
+__global__ __launch_bounds__(256) void conv_prompt_kernel(ConvArgs a) {
+    constexpr int V = Tok<BF>::V;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int block = blockIdx.x / a.blocks_c;
+    const int c = ((int)(blockIdx.x - block * a.blocks_c) * 64 + lane) * V;
+    const bool here = c < a.channels;
+    const int64_t cb = (int64_t)(here ? c : 0) * Tok<BF>::BYTES;
+
+    if (blockIdx.x == 0) check_seqlens(a.cu, a.seqs, a.tokens, a.err, threadIdx.x, 256);
+    if (block >= a.blocks_t) {
+        // empty sequences without carry: their state becomes zero
+        const int b = (block - a.blocks_t) * 4 + wave;
+        if (b >= a.seqs) return;
+        const Span s = sequence_span(a.cu, b, a.tokens);
+        const int slot = state_row(a.state, a.slots, b, a.n_slots, a.err);
+        if (s.begin == s.end && slot >= 0 && here) {
+#pragma unroll
+            for (int i = 0; i < K - 1; ++i)
+                *(uint4 *)(a.state + ((int64_t)slot * (K - 1) + i) * a.channels * Tok<BF>::BYTES + cb) = fill16(0u);
+        }
+        return;
+    }
+
+    const int64_t t0 = ((int64_t)block * 4 + wave) * RUN;
+    if (t0 >= a.tokens) return;
+    const int64_t t1 = min(t0 + RUN, a.tokens);
+    uint4 rows[RUN + K - 1];                    // input rows t0 - (K-1) .. t0 + RUN - 1
+#pragma unroll
+    for (int i = 0; i < RUN + K - 1; ++i) {
+        const int64_t t = min(max(t0 - (K - 1) + i, (int64_t)0), a.tokens - 1);
+        rows[i] = *(const uint4 *)(a.x + t * a.x_stride + cb);
+    }
+    float w[V][K], bias[V];
+    load_params<K, BF>(a, here ? c : 0, w, bias);
+
+    int b = find_sequence(a.cu, a.seqs, t0, lane);
+    Span s{0, 0};
+    int64_t next = a.tokens;                    // the next sequence's first token
+    auto enter = [&]() {
+        if (b >= 0) s = sequence_span(a.cu, b, a.tokens);
+        next = b + 1 < a.seqs ? (int64_t)a.cu[b + 1] : a.tokens;
+    };
+    enter();
+#pragma unroll
+    for (int i = 0; i < RUN; ++i) {
+        const int64_t t = t0 + i;
+        if (t >= t1) break;
+        while (t >= next && b + 1 < a.seqs) {
+            ++b;
+            enter();
+        }
+        if (b < 0 || t >= s.end || t < s.begin) continue;      // belongs to no sequence
+        const int64_t pos = t - s.begin;
+        if (pos >= K - 1) {
+            if (here) emit<K, BF, OBF>(a, a.out + t * a.out_stride + (int64_t)c * Tok<OBF>::BYTES, rows + i, w, bias);
+        } else if (pos == 0) {
+            const int slot = state_row(a.state, a.slots, b, a.n_slots, a.err);
+            if (here) {
+                const int64_t n = s.end - s.begin;
+                for (int j = 0; j < K - 1 && j < n; ++j)
+                    emit_first<K, BF, OBF>(a, t + j, s.begin, slot, cb, w, bias, c);
+                if (slot >= 0) {
+                    uint4 keep[K - 1];
+#pragma unroll
+                    for (int j = 0; j < K - 1; ++j) {
+                        const int64_t at = n - (K - 1) + j;    // place in the sequence
+                        keep[j] = at >= 0 ? *(const uint4 *)(a.x + (s.begin + at) * a.x_stride + cb)
+                                          : old_row<K, BF>(a, slot, (int)(K - 1 + at), cb);
+                    }
+#pragma unroll
+                    for (int j = 0; j < K - 1; ++j)
+                        *(uint4 *)(a.state + ((int64_t)slot * (K - 1) + j) * a.channels * Tok<BF>::BYTES + cb) = keep[j];
+                }
+            }
+        }
+    }
+}
+
+template <int K, bool BF, bool OBF>
+__global__ __launch_bounds__(256) void conv_step_kernel(ConvArgs a) {
+    constexpr int V = Tok<BF>::V;
+    const int b = blockIdx.x / a.blocks_c;
+    const int c = ((int)(blockIdx.x - b * a.blocks_c) * 256 + (int)threadIdx.x) * V;
+    if (c >= a.channels) return;
+    const int64_t cb = (int64_t)c * Tok<BF>::BYTES;
+    const int slot = state_row(a.state, a.slots, b, a.n_slots, a.err);
+    uint4 rows[K];
+    rows[K - 1] = *(const uint4 *)(a.x + (int64_t)b * a.x_stride + cb);
+#pragma unroll
+    for (int i = 0; i < K - 1; ++i) rows[i] = old_row<K, BF>(a, slot, i, cb);
+    float w[V][K], bias[V];
+    load_params<K, BF>(a, c, w, bias);
+    if (slot >= 0) {
+#pragma unroll
+        for (int i = 0; i < K - 1; ++i)
+            *(uint4 *)(a.state + ((int64_t)slot * (K - 1) + i) * a.channels * Tok<BF>::BYTES + cb) = rows[i + 1];
+    }
+    emit<K, BF, OBF>(a, a.out + (int64_t)b * a.out_stride + (int64_t)c * Tok<OBF>::BYTES, rows, w, bias);
+}
+
+ConvArgs conv_args(const lq_conv &c) {
+    ConvArgs a;
+    a.x = (const char *)c.x;
+    a.weight = c.weight;
+    a.bias = c.bias;
+    a.out = (char *)c.out;
+    a.state = (char *)c.state;
+    a.cu = c.cu_seqlens;
+    a.slots = c.slots;
+    a.err = c.err;
+    a.tokens = c.tokens;
+    a.x_stride = c.x_stride * (c.dtype == LQ_TOKEN_BF16 ? 2 : 4);
+    a.out_stride = c.out_stride * (c.out_dtype == LQ_TOKEN_BF16 ? 2 : 4);
+    a.seqs = c.seqs;
+    a.channels = c.channels;
+    a.n_slots = c.n_slots;
+    a.silu = c.silu;
+    a.carry = c.carry;
+    return a;
+}
+
+template <int K, bool BF, bool OBF>
+hipError_t launch(ConvArgs a, bool step, hipStream_t st) {
+    const int per = (step ? 256 : 64) * Tok<BF>::V;
+    a.blocks_c = (a.channels + per - 1) / per;
+    if (step) {
+        a.carry = 1;
+        hipLaunchKernelGGL((conv_step_kernel<K, BF, OBF>), dim3(a.blocks_c * a.seqs), dim3(256), 0, st, a);
+    } else {
+        a.blocks_t = (int)((a.tokens + 4 * RUN - 1) / (4 * RUN));
+        const int extra = a.state && !a.carry ? (a.seqs + 3) / 4 : 0;
+        if (a.blocks_t + extra == 0) return hipSuccess;
+        hipLaunchKernelGGL((conv_prompt_kernel<K, BF, OBF>), dim3(a.blocks_c * (a.blocks_t + extra)), dim3(256), 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+template <int K>
+hipError_t launch_types(const lq_conv &c, bool step, hipStream_t st) {
+    const ConvArgs a = conv_args(c);
+    const bool obf = c.out_dtype == LQ_TOKEN_BF16;
+    if (c.dtype == LQ_TOKEN_BF16)
+        return obf ? launch<K, true, true>(a, step, st) : launch<K, true, false>(a, step, st);
+    return obf ? launch<K, false, true>(a, step, st) : launch<K, false, false>(a, step, st);
+}
+
+hipError_t launch_width(const lq_conv &c, bool step, hipStream_t st) {
+    switch (c.width) {
+        case 2: return launch_types<2>(c, step, st);
+        case 3: return launch_types<3>(c, step, st);
+        default: return launch_types<4>(c, step, st);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_conv_prompt(const lq_conv &c, hipStream_t st) { return launch_width(c, false, st); }
+hipError_t launch_conv_step(const lq_conv &c, hipStream_t st) { return launch_width(c, true, st); }
+
+}  // namespace lq

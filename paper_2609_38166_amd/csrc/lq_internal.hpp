@@ -44,4 +44,17 @@ hipError_t launch_tile(const lq_dims &d, const StatePtrs &s, int mode, const flo
 hipError_t launch_baseline(const lq_dims &d, void *S, int state_dtype, const TokenPtrs &t,
                            hipStream_t st);
 
+// layer operators (the structs are checked by the C ABI layer before they get here)
+hipError_t launch_conv_prompt(const lq_conv &c, hipStream_t st);
+hipError_t launch_conv_step(const lq_conv &c, hipStream_t st);
+hipError_t launch_qk_norm(const lq_qk &n, hipStream_t st);
+size_t scan_workspace_bytes(const lq_dims &d, const lq_scan &s);
+hipError_t launch_scan_prompt(const lq_dims &d, const lq_scan &s, hipStream_t st);
+hipError_t launch_scan_step(const lq_dims &d, const lq_scan &s, hipStream_t st);
+hipError_t launch_scan_gates(const lq_dims &d, const lq_scan &s, float *alpha, float *beta, hipStream_t st);
+
+// host checks shared by the C ABI's source files (lq_api.hip)
+int32_t check_dims(const lq_dims *d);
+int32_t hip_status(hipError_t e);
+
 }  // namespace lq
