@@ -25,70 +25,632 @@ __device__ __forceinline__ void load8(const char *p, float *f) {
     if (!BF) unpack16<BF>(((const uint4 *)p)[1], f + 4);
 }
 
-// One workgroup per (sequence, value head): the state lies in registers, 8 key
-// channels of the value channels r0 + 16 m per thread, and the tokens follow
-// one another.  STEP: one token per request, from the dense state in place.
-template <bool STEP, bool BF, bool SBF>
-__global__ __launch_bounds__(NT) void scan_tokens_kernel(ScanArgs a) {
+// ---- single tokens ------------------------------------------------------------
+//
+// Bound: HBM, the state read and written once.  One workgroup per (request,
+// value head); 16 lanes hold a row of S^T (8 key channels each), so the output's
+// sum is a DPP row sum.
+template <bool BF, bool SBF>
+__global__ __launch_bounds__(NT) void scan_step_kernel(ScanArgs a) {
     const int tid = threadIdx.x, l16 = tid & 15, r0 = tid >> 4;
     const int b = blockIdx.x / a.heads_v, h = blockIdx.x - b * a.heads_v;
     const int slot = state_row(a.state, a.slots, b, a.n_slots, a.err);
-    Span sp{b, b + 1};
-    if (!STEP) {
-        if (blockIdx.x == 0) check_seqlens(a.cu, a.batch, a.tokens, a.err, tid, NT);
-        sp = sequence_span(a.cu, b, a.tokens);
-    }
     float s[8][8];
     char *St = a.state + ((int64_t)slot * a.heads_v + h) * D * D * (SBF ? 2 : 4);
-    const bool from = slot >= 0 && (STEP || a.carry);
     const float fill = slot == BAD_SLOT ? nanf32() : 0.0f;
 #pragma unroll
     for (int m = 0; m < 8; ++m) {
-        if (from) {
+        if (slot >= 0) {
             load8<SBF>(St + ((r0 + 16 * m) * D + 8 * l16) * (SBF ? 2 : 4), s[m]);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[m][j] = fill;
         }
     }
-    const float A = a.A[h], bias = a.bias ? a.bias[h] : 0.0f, skip = a.skip ? a.skip[h] : 0.0f;
     const int64_t kc = ((int64_t)(h / a.group) * D + 8 * l16) * Tok<BF>::BYTES;
-    for (int64_t t = sp.begin; t < sp.end; ++t) {
-        float k[8], q[8];
-        load8<BF>(a.k + t * a.k_stride + kc, k);
-        load8<BF>(a.q + t * a.q_stride + kc, q);
-        const float delta = scan_delta(load_tok<BF>(a.dt + t * a.dt_stride, h) + bias, a.softplus);
-        const float alpha = scan_alpha(delta * A);
+    float k[8], q[8];
+    load8<BF>(a.k + (int64_t)b * a.k_stride + kc, k);
+    load8<BF>(a.q + (int64_t)b * a.q_stride + kc, q);
+    const float bias = a.bias ? a.bias[h] : 0.0f;
+    const float delta = scan_delta(load_tok<BF>(a.dt + (int64_t)b * a.dt_stride, h) + bias, a.softplus);
+    const float alpha = scan_alpha(delta * a.A[h]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) k[j] *= delta;
+    for (int j = 0; j < 8; ++j) k[j] *= delta;
 #pragma unroll
-        for (int m = 0; m < 8; ++m) {
-            const int row = r0 + 16 * m;
-            const float v = load_tok<BF>(a.v + t * a.v_stride, (int64_t)h * D + row);
-            float y = 0.0f;
+    for (int m = 0; m < 8; ++m) {
+        const int row = r0 + 16 * m;
+        const float v = load_tok<BF>(a.v + (int64_t)b * a.v_stride, (int64_t)h * D + row);
+        float y = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[m][j] = fmaf(k[j], v, alpha * s[m][j]);
-            if (SBF) {
+        for (int j = 0; j < 8; ++j) s[m][j] = fmaf(k[j], v, alpha * s[m][j]);
+        if (SBF) {                                   // the output reads the state as it is stored
 #pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const uint32_t w = pk_bf16(s[m][j], s[m][j + 1]);
-                    s[m][j] = __uint_as_float(w << 16);
-                    s[m][j + 1] = __uint_as_float(w & 0xFFFF0000u);
-                }
+            for (int j = 0; j < 8; j += 2) {
+                const uint32_t w = pk_bf16(s[m][j], s[m][j + 1]);
+                s[m][j] = __uint_as_float(w << 16);
+                s[m][j + 1] = __uint_as_float(w & 0xFFFF0000u);
             }
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y = fmaf(s[m][j], q[j], y);
-            y = row16_sum(y) + (a.skip ? skip * v : 0.0f);
-            if (l16 == 0) {
-                if (BF) ((uint16_t *)(a.o + t * a.o_stride))[h * D + row] = (uint16_t)pk_bf16(y, y);
-                else ((float *)(a.o + t * a.o_stride))[h * D + row] = y;
-            }
+        for (int j = 0; j < 8; ++j) y = fmaf(s[m][j], q[j], y);
+        y = row16_sum(y) + (a.skip ? a.skip[h] * v : 0.0f);
+        if (l16 == 0) {
+            char *o = a.o + (int64_t)b * a.o_stride;
+            if (BF) ((uint16_t *)o)[h * D + row] = (uint16_t)pk_bf16(y, y);
+            else ((float *)o)[h * D + row] = y;
         }
     }
     if (slot >= 0) {
 #pragma unroll
         for (int m = 0; m < 8; ++m) store_tok<SBF, 8>(St + ((r0 + 16 * m) * D + 8 * l16) * (SBF ? 2 : 4), s[m]);
     }
+}
+
+// ---- prompts --------------------------------------------------------------------
+//
+// A chunk of C tokens at a time, on the matrix cores.  With G_t the sum of the
+// log decays from the chunk's start (base 2, fp64: differences of G are what
+// counts, and one strong decay must not blur the weak ones after it),
+//   o_t = 2^G_t S0^T q_t + sum_{j <= t} P_tj v_j + skip v_t,
+//   P_tj = 2^(G_t - G_j) delta_j (q_t . k_j),
+//   S   = 2^G_C S0 + sum_j k_j (w_j v_j)^T,   w_j = 2^(G_C - G_j) delta_j.
+//
+// One workgroup (4 waves) walks a segment of one head's tokens.  Wave w owns the
+// value channels 32 w .. 32 w + 31 and all key channels of the state, which stays
+// in registers as the accumulator of the last product.  An accumulator tile has
+// its column in the lane and 4 rows in registers, an operand its outer index in
+// the lane and 8 (bf16) or 1 (fp32) reduction slots: with its rows dealt right
+// (state_channel below) a pair of state tiles is an operand as it stands and
+// never goes through LDS.  Queries, keys and values lie in LDS as they come,
+// token by token; where a product sums over tokens, the transposing LDS read
+// turns them.
+//
+// bf16 tokens are exact operands.  What is multiplied with them in fp32 (the
+// state, P, w v) is split into bf16 terms: two for the output (2^-17, it is
+// rounded to bf16 anyway), three for the state (2^-25), which stays fp32.
+// fp32 tokens go through the fp32 matrix instructions.
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+enum Mode {
+    WHOLE = 0,      // one segment per sequence: state in, state out
+    PARTS = 1,      // segments' own sums from zero, and their decays
+    OUTPUT = 2      // outputs of segments whose start states are known
+};
+
+struct PromptArgs {
+    ScanArgs s;
+    float *parts;       // [segments][heads_v][D][D] (S^T): a segment's own sum, then its start state
+    float *decays;      // [segments][heads_v]
+    int32_t length;     // tokens of a segment
+    int32_t segments;   // upper bound of their number (WHOLE: sequences)
+    int32_t heads_k;
+};
+
+template <bool BF> struct Chunk {
+    static constexpr int C = BF ? 64 : 32;          // tokens
+    static constexpr int TILES = C / 16;
+    static constexpr int PIECES = BF ? 16 : 32;     // 16-byte pieces of a row of q, k or v
+    static constexpr int ROW = PIECES * 16;
+    static constexpr int PROW = 128;                // bytes of a row of P: 64 bf16 or 32 fp32
+    static constexpr int PTERMS = BF ? 2 : 1;
+    struct Lds {
+        alignas(16) char k[C * ROW];
+        alignas(16) char v[C * ROW];
+        alignas(16) char q[C * ROW];
+        alignas(16) char p[PTERMS * C * PROW];
+        alignas(16) double g[C];                    // G_t
+        alignas(16) float eg[C];                    // 2^G_t
+        alignas(16) float delta[C];
+        alignas(16) float w[C];
+        int found[4];
+    };
+    // Place of a piece of a row: one piece of 16 rows lies in 16 different places
+    // of a 256-byte line of banks, and so do the 4 pieces of 4 rows that a
+    // transposing read (or a column read of fp32) takes at once.
+    __device__ static __forceinline__ int at(int row, int piece) {
+        const int f = BF ? 4 * (row & 3) + ((row >> 2) & 3) : 4 * (row & 7) + ((row >> 3) & 3);
+        return row * ROW + ((piece ^ f) << 4);
+    }
+    // ... of a piece of a row of P
+    __device__ static __forceinline__ int pat(int row, int piece) { return row * PROW + ((piece ^ (row & 7)) << 4); }
+    // Key channel of register 0 of state tile i (0..7) in lane group g, and value
+    // channel of a lane in tile u of its wave: bf16 deals rows so that tiles 2i and
+    // 2i+1 hold 8 neighbouring key channels, and u = 0, 1 8 neighbouring outputs.
+    __device__ static __forceinline__ int key_channel(int i, int g) {
+        return BF ? 32 * (i >> 1) + 8 * g + 4 * (i & 1) : 16 * i + 4 * g;
+    }
+    __device__ static __forceinline__ int value_channel(int wave, int u, int l16) {
+        return BF ? 32 * wave + 8 * (l16 >> 2) + 4 * u + (l16 & 3) : 32 * wave + 16 * u + l16;
+    }
+    // ... of output register 0 in tile u
+    __device__ static __forceinline__ int out_channel(int wave, int u, int g) {
+        return BF ? 32 * wave + 8 * g + 4 * u : 32 * wave + 16 * u + 4 * g;
+    }
+};
+
+__device__ __forceinline__ bf16x8 pack8(const float *x) {
+    const uint4 w = make_uint4(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3]), pk_bf16(x[4], x[5]), pk_bf16(x[6], x[7]));
+    return __builtin_bit_cast(bf16x8, w);
+}
+// Rounds 8 floats to bf16 and leaves in x what the rounding dropped.
+__device__ __forceinline__ bf16x8 split8(float *x) {
+    const bf16x8 hi = pack8(x);
+    float f[8];
+    unpack16<true>(__builtin_bit_cast(uint4, hi), f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] -= f[i];
+    return hi;
+}
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ bf16x8 frag(const char *p) { return *(const bf16x8 *)p; }
+__device__ __forceinline__ f32x4 frag4(const char *p) { return *(const f32x4 *)p; }
+
+// 8 rows x 16 columns of bf16 in LDS turned: the lanes of a 16-lane group pass the
+// addresses of rows l16 >> 2 (p) and 4 + (l16 >> 2) (p2), 4 columns each, and a lane
+// receives its column (4 columns of lane l16 >> 2's, number l16 & 3) of the 8 rows.
+__device__ __forceinline__ bf16x8 frag_turned(const char *p, const char *p2) {
+    typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p2);
+    const s16x8 r = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    return __builtin_bit_cast(bf16x8, r);
+}
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ double scan_add64(double x, int lane) {      // inclusive sum over the wave
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const double y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
+}
+__device__ __forceinline__ int scan_add32(int x, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
+}
+
+// Segment `seg` of the packed sequences: its sequence (found[0]; -1: none) and its
+// number within it (found[1]).  All 256 threads.
+__device__ __forceinline__ void find_segment(const ScanArgs &a, int seg, int length, int *found, int *sums) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (tid == 0) found[0] = -1;
+    int before = 0;
+    for (int base = 0; base < a.batch; base += 256) {
+        int n = 0;
+        if (base + tid < a.batch) {
+            const Span sp = sequence_span(a.cu, base + tid, a.tokens);
+            n = (int)((sp.end - sp.begin + length - 1) / length);
+        }
+        const int inc = scan_add32(n, lane);
+        if (lane == 63) sums[wave] = inc;
+        __syncthreads();
+        int off = before;
+        for (int i = 0; i < wave; ++i) off += sums[i];
+        if (seg >= off + inc - n && seg < off + inc) {
+            found[0] = base + tid;
+            found[1] = seg - (off + inc - n);
+        }
+        before += sums[0] + sums[1] + sums[2] + sums[3];
+        __syncthreads();
+        if (before > seg) break;
+    }
+}
+
+template <bool BF, int MODE>
+__global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
+    using K = Chunk<BF>;
+    constexpr int C = K::C, TILES = K::TILES;
+    __shared__ typename K::Lds lds;
+    const ScanArgs &a = p.s;
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    // Workgroups go round the 8 XCDs: the heads that read one key head sit on one
+    // of them, so its rows come from that XCD's L2.
+    const int turn = blockIdx.x >> 3;
+    const int kg = turn / a.group * 8 + (blockIdx.x & 7);
+    if (kg >= p.segments * p.heads_k) return;
+    const int seg = kg / p.heads_k, hk = kg - seg * p.heads_k;
+    const int h = hk * a.group + turn % a.group;
+
+    int b = seg;
+    int64_t begin, end;
+    if (MODE == WHOLE) {
+        if (blockIdx.x == 0) check_seqlens(a.cu, a.batch, a.tokens, a.err, tid, 256);
+        const Span sp = sequence_span(a.cu, b, a.tokens);
+        begin = sp.begin;
+        end = sp.end;
+    } else {
+        find_segment(a, seg, p.length, lds.found, (int *)lds.w);
+        b = __builtin_amdgcn_readfirstlane(lds.found[0]);
+        if (b < 0) return;
+        const Span sp = sequence_span(a.cu, b, a.tokens);
+        begin = sp.begin + (int64_t)__builtin_amdgcn_readfirstlane(lds.found[1]) * p.length;
+        end = min(begin + p.length, sp.end);
+    }
+
+    // the state: tile [i][u], registers = 4 key channels
+    f32x4 S[8][2];
+    const int slot = MODE == WHOLE ? state_row(a.state, a.slots, b, a.n_slots, a.err) : NO_SLOT;
+    float *Sp = MODE == WHOLE ? (float *)a.state + ((int64_t)slot * a.heads_v + h) * D * D
+                              : p.parts + ((int64_t)seg * a.heads_v + h) * D * D;
+    {
+        const bool from = MODE == OUTPUT || (MODE == WHOLE && slot >= 0 && a.carry);
+        const float fill = MODE == WHOLE && slot == BAD_SLOT ? nanf32() : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const float *row = Sp + K::value_channel(wave, u, l16) * D;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) S[i][u] = from ? *(const f32x4 *)(row + K::key_channel(i, g)) : f32x4{fill, fill, fill, fill};
+        }
+    }
+
+    const char *kp = a.k + (int64_t)hk * K::ROW, *qp = a.q + (int64_t)hk * K::ROW, *vp = a.v + (int64_t)h * K::ROW;
+    const float A = a.A[h], bias = a.bias ? a.bias[h] : 0.0f;
+    const float skip = MODE != PARTS && a.skip ? a.skip[h] : 0.0f;
+    const bool has_skip = MODE != PARTS && a.skip;
+    double total = 0.0;                        // log2 decay of the segment (wave 3)
+
+    // The next chunk on its way: 4 pieces of each array per thread, the step of token `lane` in wave 3.
+    uint4 rk[4], rv[4], rq[4];
+    float raw = 0.0f;
+    auto fetch = [&](int64_t t0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = tid + 256 * i, row = at / K::PIECES, piece = at % K::PIECES;
+            const int64_t t = t0 + row;
+            rk[i] = rv[i] = rq[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (t < end) {
+                rk[i] = *(const uint4 *)(kp + t * a.k_stride + 16 * piece);
+                rv[i] = *(const uint4 *)(vp + t * a.v_stride + 16 * piece);
+                if (MODE != PARTS) rq[i] = *(const uint4 *)(qp + t * a.q_stride + 16 * piece);
+            }
+        }
+        if (wave == 3) raw = lane < C && t0 + lane < end ? load_tok<BF>(a.dt + (t0 + lane) * a.dt_stride, h) : 0.0f;
+    };
+    auto put = [&](int64_t t0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = tid + 256 * i, row = at / K::PIECES, piece = at % K::PIECES;
+            *(uint4 *)(lds.k + K::at(row, piece)) = rk[i];
+            *(uint4 *)(lds.v + K::at(row, piece)) = rv[i];
+            if (MODE != PARTS) *(uint4 *)(lds.q + K::at(row, piece)) = rq[i];
+        }
+        if (wave == 3) {
+            const bool there = lane < C && t0 + lane < end;
+            const float delta = there ? scan_delta(raw + bias, a.softplus) : 0.0f;
+            // (2^-1e5 is zero in any type; a bound keeps the sums exact beside it)
+            double l = there ? (double)delta * (double)A * 1.4426950408889634074 : 0.0;
+            l = l < -1e5 ? -1e5 : l;
+            const double G = scan_add64(l, lane);
+            const double all = __shfl(G, 63);
+            total += all;
+            if (lane < C) {
+                lds.g[lane] = G;
+                lds.eg[lane] = exp2_hw((float)G);
+                lds.delta[lane] = delta;
+                lds.w[lane] = exp2_hw((float)(all - G)) * delta;
+            }
+        }
+    };
+
+    if (MODE != PARTS && BF) {
+        // tiles of P above the diagonal that the products read: zero for good
+        if (tid < 128) {
+            const int term = tid >> 6, tile = (tid >> 5) & 1, row = (tid >> 1) & 15, half = tid & 1;
+            *(uint4 *)(lds.p + term * C * K::PROW + K::pat(32 * tile + row, 4 * tile + 2 + half)) = make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+    if (begin < end) fetch(begin);
+
+    for (int64_t t0 = begin; t0 < end; t0 += C) {
+        put(t0);
+        __syncthreads();
+        if (t0 + C < end) fetch(t0 + C);
+
+        f32x4 y[TILES][2];
+        if (MODE != PARTS) {
+            // P: this wave's tiles (J, T) of the triangle, J | T << 2 in 4 bits each
+            constexpr uint64_t TABLE = BF ? 0x054A98FEDCull : 0x054ull;
+            constexpr uint32_t FIRST = BF ? 0xA8630u : 0x33210u;
+            const int i0 = (FIRST >> (4 * wave)) & 15, i1 = (FIRST >> (4 * wave + 4)) & 15;
+            for (int i = i0; i < i1; ++i) {
+                const int J = (int)(TABLE >> (4 * i)) & 3, T = (int)(TABLE >> (4 * i + 2)) & 3;
+                const int j = 16 * J + l16, t = 16 * T + l16;
+                f32x4 sc = {0.0f, 0.0f, 0.0f, 0.0f};
+                if constexpr (BF) {
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) sc = mfma(frag(lds.k + K::at(j, 4 * s + g)), frag(lds.q + K::at(t, 4 * s + g)), sc);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) {
+                        const f32x4 kf = frag4(lds.k + K::at(j, 4 * s + g)), qf = frag4(lds.q + K::at(t, 4 * s + g));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc = mfma(kf[e], qf[e], sc);
+                    }
+                }
+                const int j0 = 16 * J + 4 * g;
+                const double Gt = lds.g[t];
+                const f32x4 dl = *(const f32x4 *)(lds.delta + j0);
+                float pv[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = sc[e] * (exp2_hw((float)(Gt - lds.g[j0 + e])) * dl[e]);
+                    pv[e] = j0 + e <= t ? x : 0.0f;
+                }
+                if constexpr (BF) {
+                    const uint32_t h0 = pk_bf16(pv[0], pv[1]), h1 = pk_bf16(pv[2], pv[3]);
+                    const int to = K::pat(t, 2 * J + (g >> 1)) + 8 * (g & 1);
+                    *(uint2 *)(lds.p + to) = make_uint2(h0, h1);
+                    *(uint2 *)(lds.p + C * K::PROW + to) =
+                        make_uint2(pk_bf16(pv[0] - __uint_as_float(h0 << 16), pv[1] - __uint_as_float(h0 & 0xFFFF0000u)),
+                                   pk_bf16(pv[2] - __uint_as_float(h1 << 16), pv[3] - __uint_as_float(h1 & 0xFFFF0000u)));
+                } else {
+                    *(float4 *)(lds.p + K::pat(t, 4 * J + g)) = make_float4(pv[0], pv[1], pv[2], pv[3]);
+                }
+            }
+
+            // what the state gives: y^T = S^T q^T, then 2^G_t
+#pragma unroll
+            for (int T = 0; T < TILES; ++T) y[T][0] = y[T][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if constexpr (BF) {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    bf16x8 qf[TILES];
+#pragma unroll
+                    for (int T = 0; T < TILES; ++T) qf[T] = frag(lds.q + K::at(16 * T + l16, 4 * s + g));
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        float x[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = S[2 * s + (e >> 2)][u][e & 3];
+                        const bf16x8 hi = split8(x), lo = pack8(x);
+#pragma unroll
+                        for (int T = 0; T < TILES; ++T) y[T][u] = mfma(hi, qf[T], y[T][u]);
+#pragma unroll
+                        for (int T = 0; T < TILES; ++T) y[T][u] = mfma(lo, qf[T], y[T][u]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+#pragma unroll
+                    for (int T = 0; T < TILES; ++T) {
+                        const f32x4 qf = frag4(lds.q + K::at(16 * T + l16, 4 * s + g));
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) y[T][u] = mfma(S[s][u][e], qf[e], y[T][u]);
+                    }
+            }
+#pragma unroll
+            for (int T = 0; T < TILES; ++T) {
+                const float e = lds.eg[16 * T + l16];
+                y[T][0] *= e;
+                y[T][1] *= e;
+            }
+        }
+
+        // values with the token as the reduction: bf16 [u][32 tokens], fp32 [u][4 tokens] x 8
+        bf16x8 xb[2][2];
+        float xf[2][8];
+        bool odd = false;                       // a value that is not finite
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if constexpr (BF) {
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    const int row = 32 * kk + 8 * g + (l16 >> 2), piece = 4 * wave + (l16 & 3);
+                    xb[u][kk] = frag_turned(lds.v + K::at(row, piece) + 8 * u, lds.v + K::at(row + 4, piece) + 8 * u);
+                    if (MODE != PARTS) {
+                        const uint4 w = __builtin_bit_cast(uint4, xb[u][kk]);
+                        const uint32_t m = 0x7F807F80u, c = 0x00800080u;
+                        odd |= ((((w.x & m) + c) | ((w.y & m) + c) | ((w.z & m) + c) | ((w.w & m) + c)) & 0x80008000u) != 0;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    xf[u][q] = *(const float *)(lds.v + K::at(4 * q + g, 8 * wave + 4 * u + (l16 >> 2)) + 4 * (l16 & 3));
+                    if (MODE != PARTS) odd |= (__float_as_uint(xf[u][q]) & 0x7F800000u) == 0x7F800000u;
+                }
+            }
+        }
+
+        if (MODE != PARTS) {
+            __syncthreads();                    // P is there
+            if (!__any(odd)) {
+                if constexpr (BF) {
+#pragma unroll
+                    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                        for (int T = 2 * kk; T < TILES; ++T)
+#pragma unroll
+                            for (int term = 0; term < 2; ++term) {
+                                const bf16x8 pf = frag(lds.p + term * C * K::PROW + K::pat(16 * T + l16, 4 * kk + g));
+                                y[T][0] = mfma(xb[0][kk], pf, y[T][0]);
+                                y[T][1] = mfma(xb[1][kk], pf, y[T][1]);
+                            }
+                } else {
+#pragma unroll
+                    for (int T = 0; T < TILES; ++T)
+#pragma unroll
+                        for (int q = 0; q < 4 * (T + 1); ++q) {
+                            const float pf = *(const float *)(lds.p + K::pat(16 * T + l16, q) + 4 * g);
+                            y[T][0] = mfma(xf[0][q], pf, y[T][0]);
+                            y[T][1] = mfma(xf[1][q], pf, y[T][1]);
+                        }
+                }
+            } else {
+                // The products above multiply every value of a block, also by the zeros of
+                // earlier tokens: with a value that is not finite, only what a token may
+                // see is summed, value by value.
+#pragma unroll
+                for (int T = 0; T < TILES; ++T) {
+                    const int t = 16 * T + l16;
+#pragma unroll 1
+                    for (int j = 0; j <= 16 * T + 15; ++j) {
+                        float pj;
+                        if constexpr (BF) {
+                            const char *at = lds.p + K::pat(t, j >> 3) + 2 * (j & 7);
+                            pj = bf2f(*(const uint16_t *)at) + bf2f(*(const uint16_t *)(at + C * K::PROW));
+                        } else {
+                            pj = *(const float *)(lds.p + K::pat(t, j >> 2) + 4 * (j & 3));
+                        }
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int c = K::out_channel(wave, u, g) + e;
+                                const char *row = lds.v + K::at(j, c * Tok<BF>::BYTES / 16);
+                                const float x = load_tok<BF>(row, c % Tok<BF>::V);
+                                if (j <= t) y[T][u][e] = fmaf(pj, x, y[T][u][e]);
+                            }
+                    }
+                }
+            }
+            // outputs
+#pragma unroll
+            for (int T = 0; T < TILES; ++T) {
+                const int t = 16 * T + l16;
+                float out[8];
+                if (has_skip) {
+                    float x[8];
+                    if constexpr (BF) {
+                        unpack16<true>(*(const uint4 *)(lds.v + K::at(t, 4 * wave + g)), x);
+                    } else {
+                        unpack16<false>(*(const uint4 *)(lds.v + K::at(t, 8 * wave + g)), x);
+                        unpack16<false>(*(const uint4 *)(lds.v + K::at(t, 8 * wave + 4 + g)), x + 4);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) out[e] = fmaf(skip, x[e], y[T][e >> 2][e & 3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) out[e] = y[T][e >> 2][e & 3];
+                }
+                if (t0 + t < end) {
+                    char *row = a.o + (t0 + t) * a.o_stride + (int64_t)h * K::ROW;
+                    if constexpr (BF) {
+                        store_tok<true, 8>(row + 2 * K::out_channel(wave, 0, g), out);
+                    } else {
+                        store_tok<false, 4>(row + 4 * K::out_channel(wave, 0, g), out);
+                        store_tok<false, 4>(row + 4 * K::out_channel(wave, 1, g), out + 4);
+                    }
+                }
+            }
+        }
+
+        // the state moves on
+        if (MODE != OUTPUT || t0 + C < end) {
+            const float keep = lds.eg[C - 1];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                S[i][0] *= keep;
+                S[i][1] *= keep;
+            }
+            if constexpr (BF) {
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    bf16x8 wx[2][3];
+                    const f32x4 w0 = *(const f32x4 *)(lds.w + 32 * kk + 8 * g), w1 = *(const f32x4 *)(lds.w + 32 * kk + 8 * g + 4);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        float x[8];
+                        unpack16<true>(__builtin_bit_cast(uint4, xb[u][kk]), x);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] *= e < 4 ? w0[e & 3] : w1[e & 3];
+                        wx[u][0] = split8(x);
+                        wx[u][1] = split8(x);
+                        wx[u][2] = pack8(x);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int row = 32 * kk + 8 * g + (l16 >> 2), piece = 4 * (i >> 1) + (l16 & 3);
+                        const bf16x8 kf = frag_turned(lds.k + K::at(row, piece) + 8 * (i & 1), lds.k + K::at(row + 4, piece) + 8 * (i & 1));
+#pragma unroll
+                        for (int term = 0; term < 3; ++term) {
+                            S[i][0] = mfma(kf, wx[0][term], S[i][0]);
+                            S[i][1] = mfma(kf, wx[1][term], S[i][1]);
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const float w = lds.w[4 * q + g];
+                    const float x0 = xf[0][q] * w, x1 = xf[1][q] * w;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float kf = *(const float *)(lds.k + K::at(4 * q + g, 4 * i + (l16 >> 2)) + 4 * (l16 & 3));
+                        S[i][0] = mfma(kf, x0, S[i][0]);
+                        S[i][1] = mfma(kf, x1, S[i][1]);
+                    }
+                }
+            }
+        }
+        __syncthreads();                        // everything of this chunk is read
+    }
+
+    if (MODE == PARTS || (MODE == WHOLE && slot >= 0)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float *row = Sp + K::value_channel(wave, u, l16) * D;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) *(f32x4 *)(row + K::key_channel(i, g)) = S[i][u];
+        }
+    }
+    if (MODE == PARTS && tid == 192) p.decays[(int64_t)seg * a.heads_v + h] = exp2_hw((float)total);
+}
+
+// Start states of the segments from their own sums, and the final state: per
+// (sequence, head) a thread walks the segments with 4 entries of the state.
+__global__ __launch_bounds__(256) void scan_join_kernel(PromptArgs p) {
+    __shared__ int sums[4];
+    const ScanArgs &a = p.s;
+    const int tid = threadIdx.x;
+    const int unit = blockIdx.x >> 4, at = ((blockIdx.x & 15) * 256 + tid) * 4;
+    const int b = unit / a.heads_v, h = unit - b * a.heads_v;
+    if (blockIdx.x == 0) check_seqlens(a.cu, a.batch, a.tokens, a.err, tid, 256);
+    int first = 0;
+    for (int i = tid; i < b; i += 256) {
+        const Span sp = sequence_span(a.cu, i, a.tokens);
+        first += (int)((sp.end - sp.begin + p.length - 1) / p.length);
+    }
+    first = __builtin_amdgcn_readlane(scan_add32(first, tid & 63), 63);
+    if ((tid & 63) == 0) sums[tid >> 6] = first;
+    __syncthreads();
+    first = sums[0] + sums[1] + sums[2] + sums[3];
+    const Span sp = sequence_span(a.cu, b, a.tokens);
+    const int last = min(first + (int)((sp.end - sp.begin + p.length - 1) / p.length), p.segments);
+    const int slot = state_row(a.state, a.slots, b, a.n_slots, a.err);
+    float *St = (float *)a.state + ((int64_t)slot * a.heads_v + h) * D * D + at;
+    f32x4 S = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (slot == BAD_SLOT) S = S + nanf32();
+    else if (slot >= 0 && a.carry) S = *(const f32x4 *)St;
+    const int64_t step = (int64_t)a.heads_v * D * D;
+    float *part = p.parts + ((int64_t)first * a.heads_v + h) * D * D + at;
+    const float *decay = p.decays + (int64_t)first * a.heads_v + h;
+    for (int s = first; s < last; ++s, part += step, decay += a.heads_v) {
+        const f32x4 own = *(const f32x4 *)part;
+        *(f32x4 *)part = S;
+        S = S * *decay + own;
+    }
+    if (slot >= 0) *(f32x4 *)St = S;
 }
 
 template <bool BF>
@@ -132,16 +694,62 @@ ScanArgs scan_args(const lq_dims &d, const lq_scan &s) {
     return a;
 }
 
+// How a prompt's work is split.  A sequence's chunks follow one another, so a
+// launch has one workgroup per (sequence, head) unless the sequences are cut
+// into segments, which costs a second pass over keys and values and the
+// segments' states (64 KiB each, written, joined and read).
+struct Split {
+    int32_t length;         // 0: not cut
+    int64_t segments;
+    size_t bytes;
+};
+Split split_of(const lq_dims &d, const lq_scan &s) {
+    constexpr int64_t FULL = 512;               // two workgroups on each of the 256 CUs
+    constexpr int64_t LEAST = 256;              // tokens that a segment is worth
+    Split r{0, d.batch, 0};
+    const int64_t longest = s.max_len > 0 && s.max_len < s.tokens ? s.max_len : s.tokens;
+    const int64_t units = (int64_t)d.batch * d.heads_v;
+    if (units >= FULL || longest <= 2 * LEAST) return r;
+    int64_t length = (s.tokens * d.heads_v / FULL + 63) / 64 * 64;
+    if (length < LEAST) length = LEAST;
+    if (length >= longest) return r;
+    r.length = (int32_t)length;
+    r.segments = s.tokens / length + d.batch;   // each sequence's last segment may be short
+    r.bytes = (size_t)r.segments * d.heads_v * (D * D + 4) * sizeof(float);
+    return r;
+}
+
+template <bool BF>
+hipError_t launch_prompt(const lq_dims &d, const lq_scan &s, hipStream_t st) {
+    const Split sp = split_of(d, s);
+    PromptArgs p;
+    p.s = scan_args(d, s);
+    p.heads_k = d.heads_k;
+    p.length = sp.length;
+    p.segments = (int32_t)sp.segments;
+    p.parts = (float *)s.workspace;
+    p.decays = p.parts + sp.segments * d.heads_v * D * D;
+    const int64_t groups = (sp.segments * d.heads_k + 7) / 8 * 8;
+    const dim3 grid((unsigned)(groups * p.s.group));
+    if (!sp.length) {
+        hipLaunchKernelGGL((scan_prompt_kernel<BF, WHOLE>), grid, dim3(256), 0, st, p);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((scan_prompt_kernel<BF, PARTS>), grid, dim3(256), 0, st, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(scan_join_kernel, dim3(16 * d.batch * d.heads_v), dim3(256), 0, st, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipLaunchKernelGGL((scan_prompt_kernel<BF, OUTPUT>), grid, dim3(256), 0, st, p);
+    return hipGetLastError();
+}
+
 }  // namespace
 
-size_t scan_workspace_bytes(const lq_dims &, const lq_scan &) { return 0; }
+size_t scan_workspace_bytes(const lq_dims &d, const lq_scan &s) { return split_of(d, s).bytes; }
 
 hipError_t launch_scan_prompt(const lq_dims &d, const lq_scan &s, hipStream_t st) {
-    const ScanArgs a = scan_args(d, s);
-    const dim3 grid(d.batch * d.heads_v);
-    if (s.dtype == LQ_TOKEN_BF16) hipLaunchKernelGGL((scan_tokens_kernel<false, true, false>), grid, dim3(NT), 0, st, a);
-    else hipLaunchKernelGGL((scan_tokens_kernel<false, false, false>), grid, dim3(NT), 0, st, a);
-    return hipGetLastError();
+    return s.dtype == LQ_TOKEN_BF16 ? launch_prompt<true>(d, s, st) : launch_prompt<false>(d, s, st);
 }
 
 hipError_t launch_scan_step(const lq_dims &d, const lq_scan &s, hipStream_t st) {
@@ -149,11 +757,11 @@ hipError_t launch_scan_step(const lq_dims &d, const lq_scan &s, hipStream_t st) 
     const dim3 grid(d.batch * d.heads_v);
     const bool sbf = s.state_dtype == LQ_STATE_BF16;
     if (s.dtype == LQ_TOKEN_BF16) {
-        if (sbf) hipLaunchKernelGGL((scan_tokens_kernel<true, true, true>), grid, dim3(NT), 0, st, a);
-        else hipLaunchKernelGGL((scan_tokens_kernel<true, true, false>), grid, dim3(NT), 0, st, a);
+        if (sbf) hipLaunchKernelGGL((scan_step_kernel<true, true>), grid, dim3(NT), 0, st, a);
+        else hipLaunchKernelGGL((scan_step_kernel<true, false>), grid, dim3(NT), 0, st, a);
     } else {
-        if (sbf) hipLaunchKernelGGL((scan_tokens_kernel<true, false, true>), grid, dim3(NT), 0, st, a);
-        else hipLaunchKernelGGL((scan_tokens_kernel<true, false, false>), grid, dim3(NT), 0, st, a);
+        if (sbf) hipLaunchKernelGGL((scan_step_kernel<false, true>), grid, dim3(NT), 0, st, a);
+        else hipLaunchKernelGGL((scan_step_kernel<false, false>), grid, dim3(NT), 0, st, a);
     }
     return hipGetLastError();
 }
