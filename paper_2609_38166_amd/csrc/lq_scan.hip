@@ -99,11 +99,13 @@ __global__ __launch_bounds__(NT) void scan_step_kernel(ScanArgs a) {
 // value channels 32 w .. 32 w + 31 and all key channels of the state, which stays
 // in registers as the accumulator of the last product.  An accumulator tile has
 // its column in the lane and 4 rows in registers, an operand its outer index in
-// the lane and 8 (bf16) or 1 (fp32) reduction slots: with its rows dealt right
-// (state_channel below) a pair of state tiles is an operand as it stands and
-// never goes through LDS.  Queries, keys and values lie in LDS as they come,
-// token by token; where a product sums over tokens, the transposing LDS read
-// turns them.
+// the lane and 8 (bf16) or 1 (fp32) reduction slots; the sums may run in any
+// order, so with rows and tokens dealt right a state tile, and a tile of P, is an
+// operand as it stands and never goes through LDS.  Every wave computes P for
+// itself (a tenth more products than sharing it out) and so waits for the others
+// once a chunk, when the next chunk's rows have arrived: queries, keys and values
+// are copied straight into LDS, one chunk ahead, token by token as they come, and
+// the transposing LDS read turns them where a product sums over tokens.
 //
 // bf16 tokens are exact operands.  What is multiplied with them in fp32 (the
 // state, P, w v) is split into bf16 terms: two for the output (2^-17, it is
@@ -131,32 +133,24 @@ struct PromptArgs {
 };
 
 template <bool BF> struct Chunk {
-    static constexpr int C = BF ? 64 : 32;          // tokens
+    static constexpr int C = BF ? 32 : 16;          // tokens
     static constexpr int TILES = C / 16;
     static constexpr int PIECES = BF ? 16 : 32;     // 16-byte pieces of a row of q, k or v
     static constexpr int ROW = PIECES * 16;
-    static constexpr int PROW = 128;                // bytes of a row of P: 64 bf16 or 32 fp32
-    static constexpr int PTERMS = BF ? 2 : 1;
-    struct Lds {
-        alignas(16) char k[C * ROW];
-        alignas(16) char v[C * ROW];
-        alignas(16) char q[C * ROW];
-        alignas(16) char p[PTERMS * C * PROW];
+    static constexpr int BYTES = C * ROW;           // 8 KiB either way
+    struct Rates {
         alignas(16) double g[C];                    // G_t
-        alignas(16) float eg[C];                    // 2^G_t
         alignas(16) float delta[C];
         alignas(16) float w[C];
-        int found[4];
     };
-    // Place of a piece of a row: one piece of 16 rows lies in 16 different places
+    // Place of a piece in its row: one piece of 16 rows lies in 16 different places
     // of a 256-byte line of banks, and so do the 4 pieces of 4 rows that a
-    // transposing read (or a column read of fp32) takes at once.
-    __device__ static __forceinline__ int at(int row, int piece) {
-        const int f = BF ? 4 * (row & 3) + ((row >> 2) & 3) : 4 * (row & 7) + ((row >> 3) & 3);
-        return row * ROW + ((piece ^ f) << 4);
+    // transposing read (rows 4 r ..) or a column read of fp32 (rows r, r + 4, ..)
+    // takes at once.
+    __device__ static __forceinline__ int place(int row, int piece) {
+        return piece ^ (BF ? 4 * (row & 3) + ((row >> 2) & 3) : row & 15);
     }
-    // ... of a piece of a row of P
-    __device__ static __forceinline__ int pat(int row, int piece) { return row * PROW + ((piece ^ (row & 7)) << 4); }
+    __device__ static __forceinline__ int at(int row, int piece) { return row * ROW + (place(row, piece) << 4); }
     // Key channel of register 0 of state tile i (0..7) in lane group g, and value
     // channel of a lane in tile u of its wave: bf16 deals rows so that tiles 2i and
     // 2i+1 hold 8 neighbouring key channels, and u = 0, 1 8 neighbouring outputs.
@@ -207,13 +201,24 @@ __device__ __forceinline__ bf16x8 frag_turned(const char *p, const char *p2) {
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-__device__ __forceinline__ double scan_add64(double x, int lane) {      // inclusive sum over the wave
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const double y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    return x;
+// Inclusive sum over the first 32 lanes of a wave.
+template <int SHIFT>
+__device__ __forceinline__ double row_shr_add(double x) {
+    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(x), 0x110 + SHIFT, 0xF, 0xF, true);
+    const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(x), 0x110 + SHIFT, 0xF, 0xF, true);
+    return x + __hiloint2double(hi, lo);
+}
+__device__ __forceinline__ double lane_value(double x, int lane) {
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), lane),
+                            __builtin_amdgcn_readlane(__double2loint(x), lane));
+}
+__device__ __forceinline__ double scan_add_32lanes(double x, int lane) {
+    x = row_shr_add<1>(x);
+    x = row_shr_add<2>(x);
+    x = row_shr_add<4>(x);
+    x = row_shr_add<8>(x);
+    const double first = lane_value(x, 15);
+    return lane >= 16 ? x + first : x;
 }
 __device__ __forceinline__ int scan_add32(int x, int lane) {
 #pragma unroll
@@ -252,10 +257,12 @@ __device__ __forceinline__ void find_segment(const ScanArgs &a, int seg, int len
 }
 
 template <bool BF, int MODE>
-__global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
+__global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
     using K = Chunk<BF>;
     constexpr int C = K::C, TILES = K::TILES;
-    __shared__ typename K::Lds lds;
+    constexpr int ARRAYS = MODE == PARTS ? 2 : 3;           // keys, values, queries
+    __shared__ __attribute__((aligned(16))) char rows[2][ARRAYS][K::BYTES];
+    __shared__ typename K::Rates rates[2];
     const ScanArgs &a = p.s;
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -276,12 +283,81 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
         begin = sp.begin;
         end = sp.end;
     } else {
-        find_segment(a, seg, p.length, lds.found, (int *)lds.w);
-        b = __builtin_amdgcn_readfirstlane(lds.found[0]);
+        int *found = (int *)&rates[0];
+        find_segment(a, seg, p.length, found, found + 2);
+        b = __builtin_amdgcn_readfirstlane(found[0]);
         if (b < 0) return;
         const Span sp = sequence_span(a.cu, b, a.tokens);
-        begin = sp.begin + (int64_t)__builtin_amdgcn_readfirstlane(lds.found[1]) * p.length;
+        begin = sp.begin + (int64_t)__builtin_amdgcn_readfirstlane(found[1]) * p.length;
         end = min(begin + p.length, sp.end);
+        __syncthreads();
+    }
+
+    // The rows of a chunk on their way into LDS, 2 KiB of each array per wave in two
+    // copies: lane by lane the pieces that belong at the lane's place.  The second
+    // copy's rows lie SECOND rows on, their pieces `turned` bytes aside.
+    constexpr int SECOND = 64 / K::PIECES;
+    const int row0 = 64 * 2 * wave / K::PIECES + lane / K::PIECES;
+    const int turned = 16 * (K::place(row0 + SECOND, lane % K::PIECES) - K::place(row0, lane % K::PIECES));
+    const int64_t stride[3] = {a.k_stride, a.v_stride, a.q_stride};
+    const char *from[ARRAYS];
+    {
+        const char *base[3] = {a.k + (int64_t)hk * K::ROW, a.v + (int64_t)h * K::ROW, a.q + (int64_t)hk * K::ROW};
+#pragma unroll
+        for (int n = 0; n < ARRAYS; ++n)
+            from[n] = base[n] + (begin + row0) * stride[n] + 16 * K::place(row0, lane % K::PIECES);
+    }
+    auto copy_chunk = [&](int buf, int left) {            // left: tokens of the segment from this chunk on
+#pragma unroll
+        for (int n = 0; n < ARRAYS; ++n) {
+            char *to = rows[buf][n] + 2048 * wave;
+            if (left >= C) {
+                dma16(from[n], lds_addr(to));
+                dma16(from[n] + SECOND * stride[n] + turned, lds_addr(to + 1024));
+            } else {
+                // past the segment's end lie other tokens, or none: zeros stand in for them
+                if (row0 < left) dma16(from[n], lds_addr(to));
+                else *(uint4 *)(to + 16 * lane) = make_uint4(0u, 0u, 0u, 0u);
+                if (row0 + SECOND < left) dma16(from[n] + SECOND * stride[n] + turned, lds_addr(to + 1024));
+                else *(uint4 *)(to + 1024 + 16 * lane) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            from[n] += C * stride[n];
+        }
+    };
+    // Steps and decays of a chunk's tokens, one per lane of wave 3.
+    const float A = a.A[h], bias = a.bias ? a.bias[h] : 0.0f;
+    double total = 0.0;                                   // log2 decay of the segment
+    auto load_step = [&](int64_t t0) -> uint32_t {        // as it lies in memory
+        uint32_t raw = 0;
+        if (lane < C && t0 + lane < end) {
+            const char *at = a.dt + (t0 + lane) * a.dt_stride;
+            raw = BF ? ((const uint16_t *)at)[h] : ((const uint32_t *)at)[h];
+        }
+        return raw;
+    };
+    auto put_rates = [&](int buf, uint32_t raw, int64_t t0) {
+        const bool there = lane < C && t0 + lane < end;
+        const float x = __uint_as_float(BF ? raw << 16 : raw);
+        const float delta = there ? scan_delta(x + bias, a.softplus) : 0.0f;
+        // (2^-1e5 is zero in any type; a bound keeps the sums exact beside it)
+        double l = there ? (double)delta * (double)A * 1.4426950408889634074 : 0.0;
+        l = l < -1e5 ? -1e5 : l;
+        const double G = scan_add_32lanes(l, lane), all = lane_value(G, C - 1);
+        total += all;
+        if (lane < C) {
+            rates[buf].g[lane] = G;
+            rates[buf].delta[lane] = delta;
+            rates[buf].w[lane] = exp2_hw((float)(all - G)) * delta;
+        }
+    };
+
+    uint32_t raw = 0;
+    if (begin < end) {
+        copy_chunk(0, (int)(end - begin));
+        if (wave == 3) {
+            put_rates(0, load_step(begin), begin);
+            raw = load_step(begin + C);
+        }
     }
 
     // the state: tile [i][u], registers = 4 key channels
@@ -290,130 +366,59 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
     float *Sp = MODE == WHOLE ? (float *)a.state + ((int64_t)slot * a.heads_v + h) * D * D
                               : p.parts + ((int64_t)seg * a.heads_v + h) * D * D;
     {
-        const bool from = MODE == OUTPUT || (MODE == WHOLE && slot >= 0 && a.carry);
+        const bool given = MODE == OUTPUT || (MODE == WHOLE && slot >= 0 && a.carry);
         const float fill = MODE == WHOLE && slot == BAD_SLOT ? nanf32() : 0.0f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const float *row = Sp + K::value_channel(wave, u, l16) * D;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) S[i][u] = from ? *(const f32x4 *)(row + K::key_channel(i, g)) : f32x4{fill, fill, fill, fill};
+            for (int i = 0; i < 8; ++i) {
+                S[i][u] = f32x4{fill, fill, fill, fill};
+                if (given) S[i][u] = *(const f32x4 *)(row + K::key_channel(i, g));
+            }
         }
     }
-
-    const char *kp = a.k + (int64_t)hk * K::ROW, *qp = a.q + (int64_t)hk * K::ROW, *vp = a.v + (int64_t)h * K::ROW;
-    const float A = a.A[h], bias = a.bias ? a.bias[h] : 0.0f;
-    const float skip = MODE != PARTS && a.skip ? a.skip[h] : 0.0f;
     const bool has_skip = MODE != PARTS && a.skip;
-    double total = 0.0;                        // log2 decay of the segment (wave 3)
+    const float skip = has_skip ? a.skip[h] : 0.0f;
 
-    // The next chunk on its way: 4 pieces of each array per thread, the step of token `lane` in wave 3.
-    uint4 rk[4], rv[4], rq[4];
-    float raw = 0.0f;
-    auto fetch = [&](int64_t t0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = tid + 256 * i, row = at / K::PIECES, piece = at % K::PIECES;
-            const int64_t t = t0 + row;
-            rk[i] = rv[i] = rq[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (t < end) {
-                rk[i] = *(const uint4 *)(kp + t * a.k_stride + 16 * piece);
-                rv[i] = *(const uint4 *)(vp + t * a.v_stride + 16 * piece);
-                if (MODE != PARTS) rq[i] = *(const uint4 *)(qp + t * a.q_stride + 16 * piece);
-            }
-        }
-        if (wave == 3) raw = lane < C && t0 + lane < end ? load_tok<BF>(a.dt + (t0 + lane) * a.dt_stride, h) : 0.0f;
-    };
-    auto put = [&](int64_t t0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = tid + 256 * i, row = at / K::PIECES, piece = at % K::PIECES;
-            *(uint4 *)(lds.k + K::at(row, piece)) = rk[i];
-            *(uint4 *)(lds.v + K::at(row, piece)) = rv[i];
-            if (MODE != PARTS) *(uint4 *)(lds.q + K::at(row, piece)) = rq[i];
-        }
-        if (wave == 3) {
-            const bool there = lane < C && t0 + lane < end;
-            const float delta = there ? scan_delta(raw + bias, a.softplus) : 0.0f;
-            // (2^-1e5 is zero in any type; a bound keeps the sums exact beside it)
-            double l = there ? (double)delta * (double)A * 1.4426950408889634074 : 0.0;
-            l = l < -1e5 ? -1e5 : l;
-            const double G = scan_add64(l, lane);
-            const double all = __shfl(G, 63);
-            total += all;
-            if (lane < C) {
-                lds.g[lane] = G;
-                lds.eg[lane] = exp2_hw((float)G);
-                lds.delta[lane] = delta;
-                lds.w[lane] = exp2_hw((float)(all - G)) * delta;
-            }
-        }
-    };
-
-    if (MODE != PARTS && BF) {
-        // tiles of P above the diagonal that the products read: zero for good
-        if (tid < 128) {
-            const int term = tid >> 6, tile = (tid >> 5) & 1, row = (tid >> 1) & 15, half = tid & 1;
-            *(uint4 *)(lds.p + term * C * K::PROW + K::pat(32 * tile + row, 4 * tile + 2 + half)) = make_uint4(0u, 0u, 0u, 0u);
-        }
-    }
-    if (begin < end) fetch(begin);
-
-    for (int64_t t0 = begin; t0 < end; t0 += C) {
-        put(t0);
+    int buf = 0;
+    for (int64_t t0 = begin; t0 < end; t0 += C, buf ^= 1) {
+        // this chunk's rows (and the next one's steps) have arrived, and nobody reads the last one's any more
+        asm volatile("s_waitcnt vmcnt(0)" : "+v"(raw)::"memory");
         __syncthreads();
-        if (t0 + C < end) fetch(t0 + C);
-
-        f32x4 y[TILES][2];
-        if (MODE != PARTS) {
-            // P: this wave's tiles (J, T) of the triangle, J | T << 2 in 4 bits each
-            constexpr uint64_t TABLE = BF ? 0x054A98FEDCull : 0x054ull;
-            constexpr uint32_t FIRST = BF ? 0xA8630u : 0x33210u;
-            const int i0 = (FIRST >> (4 * wave)) & 15, i1 = (FIRST >> (4 * wave + 4)) & 15;
-            for (int i = i0; i < i1; ++i) {
-                const int J = (int)(TABLE >> (4 * i)) & 3, T = (int)(TABLE >> (4 * i + 2)) & 3;
-                const int j = 16 * J + l16, t = 16 * T + l16;
-                f32x4 sc = {0.0f, 0.0f, 0.0f, 0.0f};
-                if constexpr (BF) {
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) sc = mfma(frag(lds.k + K::at(j, 4 * s + g)), frag(lds.q + K::at(t, 4 * s + g)), sc);
-                } else {
-#pragma unroll
-                    for (int s = 0; s < 8; ++s) {
-                        const f32x4 kf = frag4(lds.k + K::at(j, 4 * s + g)), qf = frag4(lds.q + K::at(t, 4 * s + g));
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sc = mfma(kf[e], qf[e], sc);
-                    }
-                }
-                const int j0 = 16 * J + 4 * g;
-                const double Gt = lds.g[t];
-                const f32x4 dl = *(const f32x4 *)(lds.delta + j0);
-                float pv[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = sc[e] * (exp2_hw((float)(Gt - lds.g[j0 + e])) * dl[e]);
-                    pv[e] = j0 + e <= t ? x : 0.0f;
-                }
-                if constexpr (BF) {
-                    const uint32_t h0 = pk_bf16(pv[0], pv[1]), h1 = pk_bf16(pv[2], pv[3]);
-                    const int to = K::pat(t, 2 * J + (g >> 1)) + 8 * (g & 1);
-                    *(uint2 *)(lds.p + to) = make_uint2(h0, h1);
-                    *(uint2 *)(lds.p + C * K::PROW + to) =
-                        make_uint2(pk_bf16(pv[0] - __uint_as_float(h0 << 16), pv[1] - __uint_as_float(h0 & 0xFFFF0000u)),
-                                   pk_bf16(pv[2] - __uint_as_float(h1 << 16), pv[3] - __uint_as_float(h1 & 0xFFFF0000u)));
-                } else {
-                    *(float4 *)(lds.p + K::pat(t, 4 * J + g)) = make_float4(pv[0], pv[1], pv[2], pv[3]);
-                }
+        if (t0 + C < end) {
+            copy_chunk(buf ^ 1, (int)(end - t0) - C);
+            if (wave == 3) {
+                put_rates(buf ^ 1, raw, t0 + C);
+                raw = load_step(t0 + 2 * C);
             }
+        }
+        const char *kr = rows[buf][0], *vr = rows[buf][1], *qr = rows[buf][ARRAYS - 1];
+        const typename K::Rates &rate = rates[buf];
 
-            // what the state gives: y^T = S^T q^T, then 2^G_t
+        f32x4 y[TILES][2], sc[TILES][TILES];
+        if (MODE != PARTS) {
+            // P^T's tiles (rows of keys J, columns of queries T, J <= T) and, from the same
+            // queries, what the state gives: y^T = S^T q^T
 #pragma unroll
-            for (int T = 0; T < TILES; ++T) y[T][0] = y[T][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int T = 0; T < TILES; ++T) {
+                y[T][0] = y[T][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int J = 0; J < TILES; ++J) sc[J][T] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            }
             if constexpr (BF) {
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
-                    bf16x8 qf[TILES];
+                    bf16x8 kf[TILES], qf[TILES];
 #pragma unroll
-                    for (int T = 0; T < TILES; ++T) qf[T] = frag(lds.q + K::at(16 * T + l16, 4 * s + g));
+                    for (int T = 0; T < TILES; ++T) {
+                        kf[T] = frag(kr + K::at(16 * T + l16, 4 * s + g));
+                        qf[T] = frag(qr + K::at(16 * T + l16, 4 * s + g));
+                    }
+#pragma unroll
+                    for (int T = 0; T < TILES; ++T)
+#pragma unroll
+                        for (int J = 0; J <= T; ++J) sc[J][T] = mfma(kf[J], qf[T], sc[J][T]);
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         float x[8];
@@ -421,127 +426,130 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
                         for (int e = 0; e < 8; ++e) x[e] = S[2 * s + (e >> 2)][u][e & 3];
                         const bf16x8 hi = split8(x), lo = pack8(x);
 #pragma unroll
-                        for (int T = 0; T < TILES; ++T) y[T][u] = mfma(hi, qf[T], y[T][u]);
-#pragma unroll
-                        for (int T = 0; T < TILES; ++T) y[T][u] = mfma(lo, qf[T], y[T][u]);
+                        for (int T = 0; T < TILES; ++T) {
+                            y[T][u] = mfma(hi, qf[T], y[T][u]);
+                            y[T][u] = mfma(lo, qf[T], y[T][u]);
+                        }
                     }
                 }
             } else {
 #pragma unroll
-                for (int s = 0; s < 8; ++s)
+                for (int s = 0; s < 8; ++s) {
+                    const f32x4 kf = frag4(kr + K::at(l16, 4 * s + g)), qf = frag4(qr + K::at(l16, 4 * s + g));
 #pragma unroll
-                    for (int T = 0; T < TILES; ++T) {
-                        const f32x4 qf = frag4(lds.q + K::at(16 * T + l16, 4 * s + g));
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) y[T][u] = mfma(S[s][u][e], qf[e], y[T][u]);
+                    for (int e = 0; e < 4; ++e) {
+                        sc[0][0] = mfma(kf[e], qf[e], sc[0][0]);
+                        y[0][0] = mfma(S[s][0][e], qf[e], y[0][0]);
+                        y[0][1] = mfma(S[s][1][e], qf[e], y[0][1]);
                     }
+                }
             }
+            // 2^G_t on what the state gives, P's weights on the tiles
 #pragma unroll
             for (int T = 0; T < TILES; ++T) {
-                const float e = lds.eg[16 * T + l16];
+                const double Gt = rate.g[16 * T + l16];
+                const float e = exp2_hw((float)Gt);
                 y[T][0] *= e;
                 y[T][1] *= e;
+#pragma unroll
+                for (int J = 0; J <= T; ++J) {
+                    const int j0 = 16 * J + 4 * g;
+                    const f32x4 dl = *(const f32x4 *)(rate.delta + j0);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float x = sc[J][T][r] * (exp2_hw((float)(Gt - rate.g[j0 + r])) * dl[r]);
+                        sc[J][T][r] = J < T || 4 * g + r <= l16 ? x : 0.0f;
+                    }
+                }
             }
         }
 
-        // values with the token as the reduction: bf16 [u][32 tokens], fp32 [u][4 tokens] x 8
-        bf16x8 xb[2][2];
-        float xf[2][8];
+        // Values as operands that sum over tokens, dealt like P's tiles: slots 4 J + r of
+        // lane group g are the tokens 16 J + 4 g + r.
+        bf16x8 xb[2];
+        float xf[2][4];
         bool odd = false;                       // a value that is not finite
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             if constexpr (BF) {
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    const int row = 32 * kk + 8 * g + (l16 >> 2), piece = 4 * wave + (l16 & 3);
-                    xb[u][kk] = frag_turned(lds.v + K::at(row, piece) + 8 * u, lds.v + K::at(row + 4, piece) + 8 * u);
-                    if (MODE != PARTS) {
-                        const uint4 w = __builtin_bit_cast(uint4, xb[u][kk]);
-                        const uint32_t m = 0x7F807F80u, c = 0x00800080u;
-                        odd |= ((((w.x & m) + c) | ((w.y & m) + c) | ((w.z & m) + c) | ((w.w & m) + c)) & 0x80008000u) != 0;
-                    }
+                const int row = 4 * g + (l16 >> 2), piece = 4 * wave + (l16 & 3);
+                xb[u] = frag_turned(vr + K::at(row, piece) + 8 * u, vr + K::at(row + 16, piece) + 8 * u);
+                if (MODE != PARTS) {
+                    const uint4 w = __builtin_bit_cast(uint4, xb[u]);
+                    const uint32_t m = 0x7F807F80u, c = 0x00800080u;
+                    odd |= ((((w.x & m) + c) | ((w.y & m) + c) | ((w.z & m) + c) | ((w.w & m) + c)) & 0x80008000u) != 0;
                 }
             } else {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    xf[u][q] = *(const float *)(lds.v + K::at(4 * q + g, 8 * wave + 4 * u + (l16 >> 2)) + 4 * (l16 & 3));
-                    if (MODE != PARTS) odd |= (__float_as_uint(xf[u][q]) & 0x7F800000u) == 0x7F800000u;
+                for (int r = 0; r < 4; ++r) {
+                    xf[u][r] = *(const float *)(vr + K::at(4 * g + r, 8 * wave + 4 * u + (l16 >> 2)) + 4 * (l16 & 3));
+                    if (MODE != PARTS) odd |= (__float_as_uint(xf[u][r]) & 0x7F800000u) == 0x7F800000u;
                 }
             }
         }
 
         if (MODE != PARTS) {
-            __syncthreads();                    // P is there
             if (!__any(odd)) {
                 if constexpr (BF) {
 #pragma unroll
-                    for (int kk = 0; kk < 2; ++kk)
+                    for (int T = 0; T < 2; ++T) {
+                        float x[8];
 #pragma unroll
-                        for (int T = 2 * kk; T < TILES; ++T)
+                        for (int e = 0; e < 8; ++e) x[e] = (e >> 2) <= T ? sc[e >> 2][T][e & 3] : 0.0f;
+                        const bf16x8 hi = split8(x), lo = pack8(x);
 #pragma unroll
-                            for (int term = 0; term < 2; ++term) {
-                                const bf16x8 pf = frag(lds.p + term * C * K::PROW + K::pat(16 * T + l16, 4 * kk + g));
-                                y[T][0] = mfma(xb[0][kk], pf, y[T][0]);
-                                y[T][1] = mfma(xb[1][kk], pf, y[T][1]);
-                            }
+                        for (int u = 0; u < 2; ++u) {
+                            y[T][u] = mfma(xb[u], hi, y[T][u]);
+                            y[T][u] = mfma(xb[u], lo, y[T][u]);
+                        }
+                    }
                 } else {
 #pragma unroll
-                    for (int T = 0; T < TILES; ++T)
-#pragma unroll
-                        for (int q = 0; q < 4 * (T + 1); ++q) {
-                            const float pf = *(const float *)(lds.p + K::pat(16 * T + l16, q) + 4 * g);
-                            y[T][0] = mfma(xf[0][q], pf, y[T][0]);
-                            y[T][1] = mfma(xf[1][q], pf, y[T][1]);
-                        }
-                }
-            } else {
-                // The products above multiply every value of a block, also by the zeros of
-                // earlier tokens: with a value that is not finite, only what a token may
-                // see is summed, value by value.
-#pragma unroll
-                for (int T = 0; T < TILES; ++T) {
-                    const int t = 16 * T + l16;
-#pragma unroll 1
-                    for (int j = 0; j <= 16 * T + 15; ++j) {
-                        float pj;
-                        if constexpr (BF) {
-                            const char *at = lds.p + K::pat(t, j >> 3) + 2 * (j & 7);
-                            pj = bf2f(*(const uint16_t *)at) + bf2f(*(const uint16_t *)(at + C * K::PROW));
-                        } else {
-                            pj = *(const float *)(lds.p + K::pat(t, j >> 2) + 4 * (j & 3));
-                        }
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int c = K::out_channel(wave, u, g) + e;
-                                const char *row = lds.v + K::at(j, c * Tok<BF>::BYTES / 16);
-                                const float x = load_tok<BF>(row, c % Tok<BF>::V);
-                                if (j <= t) y[T][u][e] = fmaf(pj, x, y[T][u][e]);
-                            }
+                    for (int r = 0; r < 4; ++r) {
+                        y[0][0] = mfma(xf[0][r], sc[0][0][r], y[0][0]);
+                        y[0][1] = mfma(xf[1][r], sc[0][0][r], y[0][1]);
                     }
                 }
+            } else {
+                // The products above multiply every value of the chunk, also by the zeros of
+                // earlier tokens: with a value that is not finite, only what a token may see
+                // is summed, value by value.
+#pragma unroll
+                for (int T = 0; T < TILES; ++T)
+#pragma unroll
+                    for (int J = 0; J <= T; ++J)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll 1
+                            for (int from_g = 0; from_g < 4; ++from_g) {
+                                const float pj = __shfl(sc[J][T][r], 16 * from_g + l16);
+                                const int j = 16 * J + 4 * from_g + r;
+#pragma unroll
+                                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        const int c = K::out_channel(wave, u, g) + e;
+                                        const float x = load_tok<BF>(vr + K::at(j, c / Tok<BF>::V), c % Tok<BF>::V);
+                                        if (j <= 16 * T + l16) y[T][u][e] = fmaf(pj, x, y[T][u][e]);
+                                    }
+                            }
             }
-            // outputs
 #pragma unroll
             for (int T = 0; T < TILES; ++T) {
                 const int t = 16 * T + l16;
                 float out[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) out[e] = y[T][e >> 2][e & 3];
                 if (has_skip) {
                     float x[8];
                     if constexpr (BF) {
-                        unpack16<true>(*(const uint4 *)(lds.v + K::at(t, 4 * wave + g)), x);
+                        unpack16<true>(*(const uint4 *)(vr + K::at(t, 4 * wave + g)), x);
                     } else {
-                        unpack16<false>(*(const uint4 *)(lds.v + K::at(t, 8 * wave + g)), x);
-                        unpack16<false>(*(const uint4 *)(lds.v + K::at(t, 8 * wave + 4 + g)), x + 4);
+                        unpack16<false>(*(const uint4 *)(vr + K::at(t, 8 * wave + g)), x);
+                        unpack16<false>(*(const uint4 *)(vr + K::at(t, 8 * wave + 4 + g)), x + 4);
                     }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) out[e] = fmaf(skip, x[e], y[T][e >> 2][e & 3]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) out[e] = y[T][e >> 2][e & 3];
+                    for (int e = 0; e < 8; ++e) out[e] = fmaf(skip, x[e], out[e]);
                 }
                 if (t0 + t < end) {
                     char *row = a.o + (t0 + t) * a.o_stride + (int64_t)h * K::ROW;
@@ -557,53 +565,49 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
 
         // the state moves on
         if (MODE != OUTPUT || t0 + C < end) {
-            const float keep = lds.eg[C - 1];
+            const float keep = exp2_hw((float)rate.g[C - 1]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 S[i][0] *= keep;
                 S[i][1] *= keep;
             }
             if constexpr (BF) {
+                bf16x8 wx[2][3];
+                const f32x4 w0 = *(const f32x4 *)(rate.w + 4 * g), w1 = *(const f32x4 *)(rate.w + 16 + 4 * g);
 #pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    bf16x8 wx[2][3];
-                    const f32x4 w0 = *(const f32x4 *)(lds.w + 32 * kk + 8 * g), w1 = *(const f32x4 *)(lds.w + 32 * kk + 8 * g + 4);
+                for (int u = 0; u < 2; ++u) {
+                    float x[8];
+                    unpack16<true>(__builtin_bit_cast(uint4, xb[u]), x);
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        float x[8];
-                        unpack16<true>(__builtin_bit_cast(uint4, xb[u][kk]), x);
+                    for (int e = 0; e < 8; ++e) x[e] *= e < 4 ? w0[e & 3] : w1[e & 3];
+                    wx[u][0] = split8(x);
+                    wx[u][1] = split8(x);
+                    wx[u][2] = pack8(x);
+                }
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] *= e < 4 ? w0[e & 3] : w1[e & 3];
-                        wx[u][0] = split8(x);
-                        wx[u][1] = split8(x);
-                        wx[u][2] = pack8(x);
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    const int row = 4 * g + (l16 >> 2), piece = 4 * (i >> 1) + (l16 & 3);
+                    const bf16x8 kf = frag_turned(kr + K::at(row, piece) + 8 * (i & 1), kr + K::at(row + 16, piece) + 8 * (i & 1));
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int row = 32 * kk + 8 * g + (l16 >> 2), piece = 4 * (i >> 1) + (l16 & 3);
-                        const bf16x8 kf = frag_turned(lds.k + K::at(row, piece) + 8 * (i & 1), lds.k + K::at(row + 4, piece) + 8 * (i & 1));
-#pragma unroll
-                        for (int term = 0; term < 3; ++term) {
-                            S[i][0] = mfma(kf, wx[0][term], S[i][0]);
-                            S[i][1] = mfma(kf, wx[1][term], S[i][1]);
-                        }
+                    for (int term = 0; term < 3; ++term) {
+                        S[i][0] = mfma(kf, wx[0][term], S[i][0]);
+                        S[i][1] = mfma(kf, wx[1][term], S[i][1]);
                     }
                 }
             } else {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const float w = lds.w[4 * q + g];
-                    const float x0 = xf[0][q] * w, x1 = xf[1][q] * w;
+                for (int r = 0; r < 4; ++r) {
+                    const float w = rate.w[4 * g + r];
+                    const float x0 = xf[0][r] * w, x1 = xf[1][r] * w;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float kf = *(const float *)(lds.k + K::at(4 * q + g, 4 * i + (l16 >> 2)) + 4 * (l16 & 3));
+                        const float kf = *(const float *)(kr + K::at(4 * g + r, 4 * i + (l16 >> 2)) + 4 * (l16 & 3));
                         S[i][0] = mfma(kf, x0, S[i][0]);
                         S[i][1] = mfma(kf, x1, S[i][1]);
                     }
                 }
             }
         }
-        __syncthreads();                        // everything of this chunk is read
     }
 
     if (MODE == PARTS || (MODE == WHOLE && slot >= 0)) {
