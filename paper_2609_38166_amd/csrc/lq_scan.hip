@@ -138,6 +138,8 @@ template <bool BF> struct Chunk {
     static constexpr int PIECES = BF ? 16 : 32;     // 16-byte pieces of a row of q, k or v
     static constexpr int ROW = PIECES * 16;
     static constexpr int BYTES = C * ROW;           // 8 KiB either way
+    static constexpr int GROUP = 4;                 // chunks whose steps and decays are prepared at once
+    static constexpr int WAVES = GROUP * C / 64;    // ... by so many waves, the waves in turn
     struct Rates {
         alignas(16) double g[C];                    // G_t
         alignas(16) float delta[C];
@@ -201,7 +203,7 @@ __device__ __forceinline__ bf16x8 frag_turned(const char *p, const char *p2) {
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Inclusive sum over the first 32 lanes of a wave.
+// Inclusive sums over each C = 16 or 32 lanes of a wave, and their totals.
 template <int SHIFT>
 __device__ __forceinline__ double row_shr_add(double x) {
     const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(x), 0x110 + SHIFT, 0xF, 0xF, true);
@@ -212,13 +214,20 @@ __device__ __forceinline__ double lane_value(double x, int lane) {
     return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), lane),
                             __builtin_amdgcn_readlane(__double2loint(x), lane));
 }
-__device__ __forceinline__ double scan_add_32lanes(double x, int lane) {
+template <int C>
+__device__ __forceinline__ double scan_add_chunk(double x, int lane, double &all) {
     x = row_shr_add<1>(x);
     x = row_shr_add<2>(x);
     x = row_shr_add<4>(x);
     x = row_shr_add<8>(x);
-    const double first = lane_value(x, 15);
-    return lane >= 16 ? x + first : x;
+    if (C == 16) {
+        all = row_bcast<15>(x);
+    } else {
+        const double first = lane < 32 ? lane_value(x, 15) : lane_value(x, 47);
+        if (lane & 16) x += first;
+        all = lane < 32 ? lane_value(x, 31) : lane_value(x, 63);
+    }
+    return x;
 }
 __device__ __forceinline__ int scan_add32(int x, int lane) {
 #pragma unroll
@@ -262,7 +271,7 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
     constexpr int C = K::C, TILES = K::TILES;
     constexpr int ARRAYS = MODE == PARTS ? 2 : 3;           // keys, values, queries
     __shared__ __attribute__((aligned(16))) char rows[2][ARRAYS][K::BYTES];
-    __shared__ typename K::Rates rates[2];
+    __shared__ typename K::Rates rates[2][K::GROUP];
     const ScanArgs &a = p.s;
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -283,7 +292,7 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
         begin = sp.begin;
         end = sp.end;
     } else {
-        int *found = (int *)&rates[0];
+        int *found = (int *)&rates[0][0];
         find_segment(a, seg, p.length, found, found + 2);
         b = __builtin_amdgcn_readfirstlane(found[0]);
         if (b < 0) return;
@@ -324,40 +333,39 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
             from[n] += C * stride[n];
         }
     };
-    // Steps and decays of a chunk's tokens, one per lane of wave 3.
+    // Steps and decays of GROUP chunks' tokens, one per lane of WAVES waves: some 250
+    // dependent instructions, so the waves take turns and are a group ahead.
+    constexpr int GROUP_TOKENS = K::GROUP * C;
     const float A = a.A[h], bias = a.bias ? a.bias[h] : 0.0f;
-    double total = 0.0;                                   // log2 decay of the segment
+    auto turn_of = [&](int group) { return wave / K::WAVES == group % (4 / K::WAVES); };
+    const int mine = 64 * (wave % K::WAVES) + lane;       // this lane's token of a group
     auto load_step = [&](int64_t t0) -> uint32_t {        // as it lies in memory
         uint32_t raw = 0;
-        if (lane < C && t0 + lane < end) {
-            const char *at = a.dt + (t0 + lane) * a.dt_stride;
+        if (t0 + mine < end) {
+            const char *at = a.dt + (t0 + mine) * a.dt_stride;
             raw = BF ? ((const uint16_t *)at)[h] : ((const uint32_t *)at)[h];
         }
         return raw;
     };
-    auto put_rates = [&](int buf, uint32_t raw, int64_t t0) {
-        const bool there = lane < C && t0 + lane < end;
+    auto put_rates = [&](int group, uint32_t raw, int64_t t0) {
+        const bool there = t0 + mine < end;
         const float x = __uint_as_float(BF ? raw << 16 : raw);
         const float delta = there ? scan_delta(x + bias, a.softplus) : 0.0f;
         // (2^-1e5 is zero in any type; a bound keeps the sums exact beside it)
         double l = there ? (double)delta * (double)A * 1.4426950408889634074 : 0.0;
         l = l < -1e5 ? -1e5 : l;
-        const double G = scan_add_32lanes(l, lane), all = lane_value(G, C - 1);
-        total += all;
-        if (lane < C) {
-            rates[buf].g[lane] = G;
-            rates[buf].delta[lane] = delta;
-            rates[buf].w[lane] = exp2_hw((float)(all - G)) * delta;
-        }
+        double all;
+        const double G = scan_add_chunk<C>(l, lane, all);
+        typename K::Rates &to = rates[group & 1][mine / C];
+        to.g[mine % C] = G;
+        to.delta[mine % C] = delta;
+        to.w[mine % C] = exp2_hw((float)(all - G)) * delta;
     };
 
     uint32_t raw = 0;
     if (begin < end) {
         copy_chunk(0, (int)(end - begin));
-        if (wave == 3) {
-            put_rates(0, load_step(begin), begin);
-            raw = load_step(begin + C);
-        }
+        if (turn_of(0)) put_rates(0, load_step(begin), begin);
     }
 
     // the state: tile [i][u], registers = 4 key channels
@@ -381,20 +389,23 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
     const bool has_skip = MODE != PARTS && a.skip;
     const float skip = has_skip ? a.skip[h] : 0.0f;
 
-    int buf = 0;
-    for (int64_t t0 = begin; t0 < end; t0 += C, buf ^= 1) {
-        // this chunk's rows (and the next one's steps) have arrived, and nobody reads the last one's any more
+    double total = 0.0;                                   // log2 decay of the segment
+    int chunk = 0;
+    for (int64_t t0 = begin; t0 < end; t0 += C, ++chunk) {
+        // this chunk's rows (and the next group's steps) have arrived, and nobody reads the last one's any more
         asm volatile("s_waitcnt vmcnt(0)" : "+v"(raw)::"memory");
         __syncthreads();
+        const int buf = chunk & 1, group = chunk / K::GROUP;
         if (t0 + C < end) {
             copy_chunk(buf ^ 1, (int)(end - t0) - C);
-            if (wave == 3) {
-                put_rates(buf ^ 1, raw, t0 + C);
-                raw = load_step(t0 + 2 * C);
+            // the next group: its steps on their way after this one's second chunk, used after its third
+            if (turn_of(group + 1)) {
+                if (chunk % K::GROUP == 1) raw = load_step(t0 + GROUP_TOKENS - C);
+                if (chunk % K::GROUP == 2) put_rates(group + 1, raw, t0 + GROUP_TOKENS - 2 * C);
             }
         }
         const char *kr = rows[buf][0], *vr = rows[buf][1], *qr = rows[buf][ARRAYS - 1];
-        const typename K::Rates &rate = rates[buf];
+        const typename K::Rates &rate = rates[group & 1][chunk % K::GROUP];
 
         f32x4 y[TILES][2], sc[TILES][TILES];
         if (MODE != PARTS) {
@@ -566,6 +577,7 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
         // the state moves on
         if (MODE != OUTPUT || t0 + C < end) {
             const float keep = exp2_hw((float)rate.g[C - 1]);
+            if (MODE == PARTS) total += rate.g[C - 1];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 S[i][0] *= keep;
@@ -618,7 +630,7 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
             for (int i = 0; i < 8; ++i) *(f32x4 *)(row + K::key_channel(i, g)) = S[i][u];
         }
     }
-    if (MODE == PARTS && tid == 192) p.decays[(int64_t)seg * a.heads_v + h] = exp2_hw((float)total);
+    if (MODE == PARTS && tid == 0) p.decays[(int64_t)seg * a.heads_v + h] = exp2_hw((float)total);
 }
 
 // Start states of the segments from their own sums, and the final state: per
