@@ -266,11 +266,13 @@ __device__ __forceinline__ void find_segment(const ScanArgs &a, int seg, int len
 }
 
 template <bool BF, int MODE>
-__global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
+__global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
     using K = Chunk<BF>;
     constexpr int C = K::C, TILES = K::TILES;
     constexpr int ARRAYS = MODE == PARTS ? 2 : 3;           // keys, values, queries
-    __shared__ __attribute__((aligned(16))) char rows[2][ARRAYS][K::BYTES];
+    constexpr int AHEAD = 2;                                // chunks on their way
+    __shared__ __attribute__((aligned(16))) char rows[AHEAD + 1][ARRAYS][K::BYTES];
+    __shared__ uint32_t steps[K::GROUP * C];                // dt of a group as it lies in memory
     __shared__ typename K::Rates rates[2][K::GROUP];
     const ScanArgs &a = p.s;
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
@@ -339,17 +341,14 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
     const float A = a.A[h], bias = a.bias ? a.bias[h] : 0.0f;
     auto turn_of = [&](int group) { return wave / K::WAVES == group % (4 / K::WAVES); };
     const int mine = 64 * (wave % K::WAVES) + lane;       // this lane's token of a group
-    auto load_step = [&](int64_t t0) -> uint32_t {        // as it lies in memory
-        uint32_t raw = 0;
-        if (t0 + mine < end) {
-            const char *at = a.dt + (t0 + mine) * a.dt_stride;
-            raw = BF ? ((const uint16_t *)at)[h] : ((const uint32_t *)at)[h];
-        }
-        return raw;
+    auto copy_steps = [&](int64_t t0) {
+        if (t0 + mine < end)
+            dma_element<Tok<BF>::BYTES>(a.dt + (t0 + mine) * a.dt_stride + h * Tok<BF>::BYTES,
+                                        lds_addr(steps + 64 * (wave % K::WAVES)));
     };
-    auto put_rates = [&](int group, uint32_t raw, int64_t t0) {
+    auto put_rates = [&](int group, int64_t t0) {
         const bool there = t0 + mine < end;
-        const float x = __uint_as_float(BF ? raw << 16 : raw);
+        const float x = __uint_as_float(BF ? steps[mine] << 16 : steps[mine]);
         const float delta = there ? scan_delta(x + bias, a.softplus) : 0.0f;
         // (2^-1e5 is zero in any type; a bound keeps the sums exact beside it)
         double l = there ? (double)delta * (double)A * 1.4426950408889634074 : 0.0;
@@ -362,10 +361,11 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
         to.w[mine % C] = exp2_hw((float)(all - G)) * delta;
     };
 
-    uint32_t raw = 0;
     if (begin < end) {
-        copy_chunk(0, (int)(end - begin));
-        if (turn_of(0)) put_rates(0, load_step(begin), begin);
+        if (turn_of(0)) copy_steps(begin);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (begin + i * C < end) copy_chunk(i, (int)(end - begin) - i * C);
     }
 
     // the state: tile [i][u], registers = 4 key channels
@@ -389,23 +389,32 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
     const bool has_skip = MODE != PARTS && a.skip;
     const float skip = has_skip ? a.skip[h] : 0.0f;
 
+    if (begin < end && turn_of(0)) {
+        wait_vm_all();
+        put_rates(0, begin);
+    }
     double total = 0.0;                                   // log2 decay of the segment
-    int chunk = 0;
+    int chunk = 0, buf = 0;
     for (int64_t t0 = begin; t0 < end; t0 += C, ++chunk) {
-        // this chunk's rows (and the next group's steps) have arrived, and nobody reads the last one's any more
-        asm volatile("s_waitcnt vmcnt(0)" : "+v"(raw)::"memory");
+        // This chunk's rows have arrived, and nobody reads the last one's any more.  Younger
+        // than its copies are the next chunk's, if that is a whole one (a wave skips copies
+        // past the segment's end), and the last chunk's output stores.
+        constexpr int COPIES = 2 * ARRAYS, STORES = MODE == PARTS ? 0 : 2;
+        if (t0 + 2 * C > end) wait_vm_all();
+        else if (chunk == 0) wait_vm<COPIES>();
+        else wait_vm<COPIES + STORES>();
         __syncthreads();
-        const int buf = chunk & 1, group = chunk / K::GROUP;
-        if (t0 + C < end) {
-            copy_chunk(buf ^ 1, (int)(end - t0) - C);
-            // the next group: its steps on their way after this one's second chunk, used after its third
-            if (turn_of(group + 1)) {
-                if (chunk % K::GROUP == 1) raw = load_step(t0 + GROUP_TOKENS - C);
-                if (chunk % K::GROUP == 2) put_rates(group + 1, raw, t0 + GROUP_TOKENS - 2 * C);
-            }
-        }
+        const int group = chunk / K::GROUP;
         const char *kr = rows[buf][0], *vr = rows[buf][1], *qr = rows[buf][ARRAYS - 1];
         const typename K::Rates &rate = rates[group & 1][chunk % K::GROUP];
+        buf = buf == AHEAD ? 0 : buf + 1;                 // the next chunk's; the one after it goes where the last one was
+        // the next group: its steps set out with this one's first chunk and are there (older
+        // than the rows of its third, which were waited for) when that begins
+        if (turn_of(group + 1)) {
+            if (chunk % K::GROUP == 0) copy_steps(t0 + GROUP_TOKENS);
+            if (chunk % K::GROUP == 2) put_rates(group + 1, t0 + GROUP_TOKENS - 2 * C);
+        }
+        if (t0 + AHEAD * C < end) copy_chunk(buf == AHEAD ? 0 : buf + 1, (int)(end - t0) - AHEAD * C);
 
         f32x4 y[TILES][2], sc[TILES][TILES];
         if (MODE != PARTS) {
