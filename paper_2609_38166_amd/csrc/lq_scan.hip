@@ -1,6 +1,8 @@
 // Selective state space scan, packed prompts and single tokens:
 //   S_t = alpha_t S_{t-1} + delta_t k_t v_t^T,   o_t = S_t^T q_t + skip v_t,
 // delta = softplus(dt + bias), alpha = exp(delta A), the state kept as S^T.
+#include <type_traits>
+
 #include "lq_layer.hpp"
 #include "lq_internal.hpp"
 
@@ -140,6 +142,7 @@ template <bool BF> struct Chunk {
     static constexpr int BYTES = C * ROW;           // 8 KiB either way
     static constexpr int GROUP = 4;                 // chunks whose steps and decays are prepared at once
     static constexpr int WAVES = GROUP * C / 64;    // ... by so many waves, the waves in turn
+    typedef typename std::conditional<BF, bf16x8, f32x4>::type Operand;    // a piece of a row
     struct Rates {
         alignas(16) double g[C];                    // G_t
         alignas(16) float delta[C];
@@ -187,8 +190,6 @@ __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
 __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ bf16x8 frag(const char *p) { return *(const bf16x8 *)p; }
-__device__ __forceinline__ f32x4 frag4(const char *p) { return *(const f32x4 *)p; }
 
 // 8 rows x 16 columns of bf16 in LDS turned: the lanes of a 16-lane group pass the
 // addresses of rows l16 >> 2 (p) and 4 + (l16 >> 2) (p2), 4 columns each, and a lane
@@ -416,8 +417,67 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
         }
         if (t0 + AHEAD * C < end) copy_chunk(buf == AHEAD ? 0 : buf + 1, (int)(end - t0) - AHEAD * C);
 
-        f32x4 y[TILES][2], sc[TILES][TILES];
+        // LDS reads set out well ahead of their use (pin() keeps them there; arithmetic may
+        // cross it): left to the compiler they stood right before it, some 20 round trips
+        // a chunk in the open.
+        auto pin = [] { __builtin_amdgcn_sched_barrier(1); };
+
+        // Values as operands that sum over tokens, dealt like P's tiles: slots 4 J + r of
+        // lane group g are the tokens 16 J + 4 g + r.
+        bf16x8 xb[2];
+        float xf[2][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if constexpr (BF) {
+                const int row = 4 * g + (l16 >> 2), piece = 4 * wave + (l16 & 3);
+                xb[u] = frag_turned(vr + K::at(row, piece) + 8 * u, vr + K::at(row + 16, piece) + 8 * u);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    xf[u][r] = *(const float *)(vr + K::at(4 * g + r, 8 * wave + 4 * u + (l16 >> 2)) + 4 * (l16 & 3));
+            }
+        }
+        f32x4 w[TILES];
+#pragma unroll
+        for (int J = 0; J < TILES; ++J) w[J] = *(const f32x4 *)(rate.w + 16 * J + 4 * g);
+        const double g_end = rate.g[C - 1];
+
+        f32x4 y[TILES][2], sc[TILES][TILES], weight[TILES][TILES];
+        float grown[TILES];
+        bool odd = false;                       // a value that is not finite
         if (MODE != PARTS) {
+            // operands of step s of the products below: keys and queries of its channels
+            typedef typename K::Operand Operand;
+            Operand kf[2][TILES], qf[2][TILES];
+            auto load_kq = [&](int s) {
+#pragma unroll
+                for (int T = 0; T < TILES; ++T) {
+                    kf[s & 1][T] = *(const Operand *)(kr + K::at(16 * T + l16, 4 * s + g));
+                    qf[s & 1][T] = *(const Operand *)(qr + K::at(16 * T + l16, 4 * s + g));
+                }
+            };
+            double gt[TILES], gj[TILES][4];
+            f32x4 dl[TILES];
+#pragma unroll
+            for (int T = 0; T < TILES; ++T) {
+                gt[T] = rate.g[16 * T + l16];
+                dl[T] = *(const f32x4 *)(rate.delta + 16 * T + 4 * g);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) gj[T][r] = rate.g[16 * T + 4 * g + r];
+            }
+            load_kq(0);
+            pin();
+
+            // P's weights and 2^G_t
+#pragma unroll
+            for (int T = 0; T < TILES; ++T) {
+                grown[T] = exp2_hw((float)gt[T]);
+#pragma unroll
+                for (int J = 0; J <= T; ++J)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) weight[J][T][r] = exp2_hw((float)(gt[T] - gj[J][r])) * dl[J][r];
+            }
+
             // P^T's tiles (rows of keys J, columns of queries T, J <= T) and, from the same
             // queries, what the state gives: y^T = S^T q^T
 #pragma unroll
@@ -426,19 +486,16 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
 #pragma unroll
                 for (int J = 0; J < TILES; ++J) sc[J][T] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             }
-            if constexpr (BF) {
+            constexpr int STEPS = BF ? 4 : 8;
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    bf16x8 kf[TILES], qf[TILES];
-#pragma unroll
-                    for (int T = 0; T < TILES; ++T) {
-                        kf[T] = frag(kr + K::at(16 * T + l16, 4 * s + g));
-                        qf[T] = frag(qr + K::at(16 * T + l16, 4 * s + g));
-                    }
+            for (int s = 0; s < STEPS; ++s) {
+                if (s + 1 < STEPS) load_kq(s + 1);
+                pin();
+                if constexpr (BF) {
 #pragma unroll
                     for (int T = 0; T < TILES; ++T)
 #pragma unroll
-                        for (int J = 0; J <= T; ++J) sc[J][T] = mfma(kf[J], qf[T], sc[J][T]);
+                        for (int J = 0; J <= T; ++J) sc[J][T] = mfma(kf[s & 1][J], qf[s & 1][T], sc[J][T]);
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         float x[8];
@@ -446,69 +503,63 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
                         for (int e = 0; e < 8; ++e) x[e] = S[2 * s + (e >> 2)][u][e & 3];
                         const bf16x8 hi = split8(x), lo = pack8(x);
 #pragma unroll
-                        for (int T = 0; T < TILES; ++T) {
-                            y[T][u] = mfma(hi, qf[T], y[T][u]);
-                            y[T][u] = mfma(lo, qf[T], y[T][u]);
-                        }
-                    }
-                }
-            } else {
+                        for (int T = 0; T < TILES; ++T) y[T][u] = mfma(hi, qf[s & 1][T], y[T][u]);
 #pragma unroll
-                for (int s = 0; s < 8; ++s) {
-                    const f32x4 kf = frag4(kr + K::at(l16, 4 * s + g)), qf = frag4(qr + K::at(l16, 4 * s + g));
+                        for (int T = 0; T < TILES; ++T) y[T][u] = mfma(lo, qf[s & 1][T], y[T][u]);
+                    }
+                } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        sc[0][0] = mfma(kf[e], qf[e], sc[0][0]);
-                        y[0][0] = mfma(S[s][0][e], qf[e], y[0][0]);
-                        y[0][1] = mfma(S[s][1][e], qf[e], y[0][1]);
-                    }
-                }
-            }
-            // 2^G_t on what the state gives, P's weights on the tiles
-#pragma unroll
-            for (int T = 0; T < TILES; ++T) {
-                const double Gt = rate.g[16 * T + l16];
-                const float e = exp2_hw((float)Gt);
-                y[T][0] *= e;
-                y[T][1] *= e;
-#pragma unroll
-                for (int J = 0; J <= T; ++J) {
-                    const int j0 = 16 * J + 4 * g;
-                    const f32x4 dl = *(const f32x4 *)(rate.delta + j0);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float x = sc[J][T][r] * (exp2_hw((float)(Gt - rate.g[j0 + r])) * dl[r]);
-                        sc[J][T][r] = J < T || 4 * g + r <= l16 ? x : 0.0f;
+                        sc[0][0] = mfma(kf[s & 1][0][e], qf[s & 1][0][e], sc[0][0]);
+                        y[0][0] = mfma(S[s][0][e], qf[s & 1][0][e], y[0][0]);
+                        y[0][1] = mfma(S[s][1][e], qf[s & 1][0][e], y[0][1]);
                     }
                 }
             }
         }
 
-        // Values as operands that sum over tokens, dealt like P's tiles: slots 4 J + r of
-        // lane group g are the tokens 16 J + 4 g + r.
-        bf16x8 xb[2];
-        float xf[2][4];
-        bool odd = false;                       // a value that is not finite
+        // keys as operands that sum over tokens, for the state
+        bf16x8 kb[8];
+        float kt[4][8];
+        if constexpr (BF) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if constexpr (BF) {
-                const int row = 4 * g + (l16 >> 2), piece = 4 * wave + (l16 & 3);
-                xb[u] = frag_turned(vr + K::at(row, piece) + 8 * u, vr + K::at(row + 16, piece) + 8 * u);
-                if (MODE != PARTS) {
-                    const uint4 w = __builtin_bit_cast(uint4, xb[u]);
-                    const uint32_t m = 0x7F807F80u, c = 0x00800080u;
-                    odd |= ((((w.x & m) + c) | ((w.y & m) + c) | ((w.z & m) + c) | ((w.w & m) + c)) & 0x80008000u) != 0;
-                }
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    xf[u][r] = *(const float *)(vr + K::at(4 * g + r, 8 * wave + 4 * u + (l16 >> 2)) + 4 * (l16 & 3));
-                    if (MODE != PARTS) odd |= (__float_as_uint(xf[u][r]) & 0x7F800000u) == 0x7F800000u;
-                }
+            for (int i = 0; i < 8; ++i) {
+                const int row = 4 * g + (l16 >> 2), piece = 4 * (i >> 1) + (l16 & 3);
+                kb[i] = frag_turned(kr + K::at(row, piece) + 8 * (i & 1), kr + K::at(row + 16, piece) + 8 * (i & 1));
             }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    kt[r][i] = *(const float *)(kr + K::at(4 * g + r, 4 * i + (l16 >> 2)) + 4 * (l16 & 3));
         }
+        pin();
 
         if (MODE != PARTS) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if constexpr (BF) {
+                    const uint4 v = __builtin_bit_cast(uint4, xb[u]);
+                    const uint32_t m = 0x7F807F80u, c = 0x00800080u;
+                    odd |= ((((v.x & m) + c) | ((v.y & m) + c) | ((v.z & m) + c) | ((v.w & m) + c)) & 0x80008000u) != 0;
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) odd |= (__float_as_uint(xf[u][r]) & 0x7F800000u) == 0x7F800000u;
+                }
+            }
+#pragma unroll
+            for (int T = 0; T < TILES; ++T) {
+                y[T][0] *= grown[T];
+                y[T][1] *= grown[T];
+#pragma unroll
+                for (int J = 0; J <= T; ++J)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float x = sc[J][T][r] * weight[J][T][r];
+                        sc[J][T][r] = J < T || 4 * g + r <= l16 ? x : 0.0f;
+                    }
+            }
             if (!__any(odd)) {
                 if constexpr (BF) {
 #pragma unroll
@@ -585,8 +636,8 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
 
         // the state moves on
         if (MODE != OUTPUT || t0 + C < end) {
-            const float keep = exp2_hw((float)rate.g[C - 1]);
-            if (MODE == PARTS) total += rate.g[C - 1];
+            const float keep = exp2_hw((float)g_end);
+            if (MODE == PARTS) total += g_end;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 S[i][0] *= keep;
@@ -594,37 +645,31 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
             }
             if constexpr (BF) {
                 bf16x8 wx[2][3];
-                const f32x4 w0 = *(const f32x4 *)(rate.w + 4 * g), w1 = *(const f32x4 *)(rate.w + 16 + 4 * g);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     float x[8];
                     unpack16<true>(__builtin_bit_cast(uint4, xb[u]), x);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] *= e < 4 ? w0[e & 3] : w1[e & 3];
+                    for (int e = 0; e < 8; ++e) x[e] *= w[e >> 2][e & 3];
                     wx[u][0] = split8(x);
                     wx[u][1] = split8(x);
                     wx[u][2] = pack8(x);
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int row = 4 * g + (l16 >> 2), piece = 4 * (i >> 1) + (l16 & 3);
-                    const bf16x8 kf = frag_turned(kr + K::at(row, piece) + 8 * (i & 1), kr + K::at(row + 16, piece) + 8 * (i & 1));
+                for (int term = 0; term < 3; ++term)
 #pragma unroll
-                    for (int term = 0; term < 3; ++term) {
-                        S[i][0] = mfma(kf, wx[0][term], S[i][0]);
-                        S[i][1] = mfma(kf, wx[1][term], S[i][1]);
+                    for (int i = 0; i < 8; ++i) {
+                        S[i][0] = mfma(kb[i], wx[0][term], S[i][0]);
+                        S[i][1] = mfma(kb[i], wx[1][term], S[i][1]);
                     }
-                }
             } else {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float w = rate.w[4 * g + r];
-                    const float x0 = xf[0][r] * w, x1 = xf[1][r] * w;
+                    const float x0 = xf[0][r] * w[0][r], x1 = xf[1][r] * w[0][r];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float kf = *(const float *)(kr + K::at(4 * g + r, 4 * i + (l16 >> 2)) + 4 * (l16 & 3));
-                        S[i][0] = mfma(kf, x0, S[i][0]);
-                        S[i][1] = mfma(kf, x1, S[i][1]);
+                        S[i][0] = mfma(kt[r][i], x0, S[i][0]);
+                        S[i][1] = mfma(kt[r][i], x1, S[i][1]);
                     }
                 }
             }
