@@ -83,7 +83,8 @@ _L = None
 # loaded, it or what stands in for it) and the addresses of the entry points it calls
 _M = None
 _FN = {"leapquant_decode_step": 0, "leapquant_decode_step_general": 0, "leapquant_decode_step_commit": 0,
-       "leapquant_window_commit": 0}
+       "leapquant_window_commit": 0, "leapquant_conv_prompt": 0, "leapquant_conv_step": 0, "leapquant_qk_norm": 0,
+       "leapquant_scan_prompt": 0, "leapquant_scan_step": 0, "leapquant_scan_workspace_bytes": 0}
 
 
 class _NoMarshal:
@@ -94,7 +95,7 @@ class _NoMarshal:
     def step(*args):
         return None
 
-    step_general = commit = step
+    step_general = commit = conv = qk_norm = scan = step
 
 
 def _load_marshal(addr):
@@ -510,6 +511,10 @@ def leapquant_conv_prompt(x, weight, out, cu_seqlens, bias=None, silu=True, stat
     """Short causal convolution of packed sequences: x, out [tokens, channels], weight
     [channels, width], cu_seqlens int32 [sequences + 1]; state [slots, width-1, channels]
     of x's type, read if `carry`, holds the last inputs afterwards."""
+    if stream is None and (_M or _lib()):
+        status = _M.conv(_FN["leapquant_conv_prompt"], x, weight, out, cu_seqlens, bias, silu, state, carry, slots, err)
+        if status is not None:
+            return _check(status, "leapquant_conv_prompt")
     seqs = _seqs(cu_seqlens)
     _conv("leapquant_conv_prompt", x, weight, out, seqs, cu_seqlens, bias, silu, state, carry, slots, err, stream)
 
@@ -518,6 +523,10 @@ def leapquant_conv_step(x, weight, out, state, bias=None, silu=True, slots=None,
     """The convolution for one token of every request (row b of x), state in place."""
     if state is None:
         raise ValueError("state is required")
+    if stream is None and (_M or _lib()):
+        status = _M.conv(_FN["leapquant_conv_step"], x, weight, out, None, bias, silu, state, True, slots, err)
+        if status is not None:
+            return _check(status, "leapquant_conv_step")
     _conv("leapquant_conv_step", x, weight, out, x.shape[0], None, bias, silu, state, True, slots, err, stream)
 
 
@@ -533,6 +542,11 @@ def leapquant_qk_norm(q, k, q_out, k_out, norm=LQ_NORM_L2, eps=1e-6, q_weight=No
     """Norm of every query and key head [tokens, heads, d] and the rotation of the first
     2 * cos.shape[1] channels by the token's position (cos, sin [positions, rot/2]); k and
     k_out may be None."""
+    if stream is None and (_M or _lib()):
+        status = _M.qk_norm(_FN["leapquant_qk_norm"], q, k, q_out, k_out, norm, eps, q_weight, k_weight, q_scale, cos, sin,
+                            positions, interleaved, err)
+        if status is not None:
+            return _check(status, "leapquant_qk_norm")
     if q.dim() != 3:
         raise ValueError("q must be [tokens, heads, d]")
     tokens, hq, d = q.shape
@@ -582,6 +596,11 @@ def leapquant_scan_prompt(dims: lq_dims, q, k, v, dt, A, o, cu_seqlens, D=None, 
     max_len, the longest sequence, lets the work be split better where it is known.  The
     workspace is allocated here unless a uint8 tensor is given; a stream of the caller's
     needs one."""
+    if stream is None and (_M or _lib()):
+        status = _M.scan(_FN["leapquant_scan_prompt"], _FN["leapquant_scan_workspace_bytes"], dims, q, k, v, dt, A, o, D, dt_bias,
+                         softplus, state, cu_seqlens, carry, slots, max_len, workspace, err)
+        if status is not None:
+            return _check(status, "leapquant_scan_prompt")
     if _seqs(cu_seqlens) != dims.batch:
         raise ValueError(f"cu_seqlens holds {_seqs(cu_seqlens)} sequences, dims.batch is {dims.batch}")
     a = _scan_args(dims, q, k, v, dt, A, o, state, cu_seqlens, D, dt_bias, softplus, carry, slots, max_len, err)
@@ -610,6 +629,11 @@ def leapquant_scan_step(dims: lq_dims, state, q, k, v, dt, A, o, D=None, dt_bias
     """The scan for one token of every request (row b), its dense state (fp32 or bf16) in place."""
     if state is None:
         raise ValueError("state is required")
+    if stream is None and (_M or _lib()):
+        status = _M.scan(_FN["leapquant_scan_step"], 0, dims, q, k, v, dt, A, o, D, dt_bias, softplus, state, None, True, slots,
+                         0, None, err)
+        if status is not None:
+            return _check(status, "leapquant_scan_step")
     a = _scan_args(dims, q, k, v, dt, A, o, state, None, D, dt_bias, softplus, True, slots, 0, err)
     _check(_lib().leapquant_scan_step(C.byref(dims), C.byref(a), _stream(stream)), "leapquant_scan_step")
 

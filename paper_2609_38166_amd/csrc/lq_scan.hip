@@ -110,8 +110,8 @@ __global__ __launch_bounds__(NT) void scan_step_kernel(ScanArgs a) {
 // the transposing LDS read turns them where a product sums over tokens.
 //
 // bf16 tokens are exact operands.  What is multiplied with them in fp32 (the
-// state, P, w v) is split into bf16 terms: two for the output (2^-17, it is
-// rounded to bf16 anyway), three for the state (2^-25), which stays fp32.
+// state, P, w v) is split into bf16 terms: two for the output (2^-16, it is
+// rounded to bf16 anyway), three for the state (2^-24), which stays fp32.
 // fp32 tokens go through the fp32 matrix instructions.
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -175,14 +175,19 @@ __device__ __forceinline__ bf16x8 pack8(const float *x) {
     const uint4 w = make_uint4(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3]), pk_bf16(x[4], x[5]), pk_bf16(x[6], x[7]));
     return __builtin_bit_cast(bf16x8, w);
 }
-// Rounds 8 floats to bf16 and leaves in x what the rounding dropped.
+// Cuts 8 floats to bf16 and leaves in x what that dropped (exact).  Cut, not rounded:
+// the upper half as it lies is the term (v_and at twice the rate of a shift, and one
+// permutation packs two), at the price of one bit of the terms together.
 __device__ __forceinline__ bf16x8 split8(float *x) {
-    const bf16x8 hi = pack8(x);
-    float f[8];
-    unpack16<true>(__builtin_bit_cast(uint4, hi), f);
+    uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] -= f[i];
-    return hi;
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t a = __float_as_uint(x[2 * i]), b = __float_as_uint(x[2 * i + 1]);
+        w[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        x[2 * i] -= __uint_as_float(a & 0xFFFF0000u);
+        x[2 * i + 1] -= __uint_as_float(b & 0xFFFF0000u);
+    }
+    return __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
 }
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);

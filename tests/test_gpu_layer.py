@@ -477,3 +477,66 @@ def test_rows_and_slots_past_32_bits():
         B.leapquant_scan_step(d, rows, y["q"][:1], y["k"][:1], y["v"][:1], y["dt"][:1], y["A"], a[:1],
                               slots=slots if rows is many else None)
     assert torch.equal(many[40000], st[0][0]) and not many[:40000].any()
+
+
+# --------------------------------------------------------------------------------------------- the native call path
+
+def test_native_path_takes_regular_calls_and_gives_the_same(monkeypatch):
+    n = 1000
+    x = scan_inputs(n, 3, 1, BF)
+    y = cu_args(x)
+    got, taken = [], []
+    assert B.lib() and B._M is not B._NoMarshal
+
+    class Native:
+        def __getattr__(self, name):
+            def call(*args):
+                status = getattr(native, name)(*args)
+                taken.append((name, status))
+                return status
+            return call
+
+    native = B._M
+    for side in (Native(), B._NoMarshal):
+        monkeypatch.setattr(B, "_M", side)
+        s = _buffers(n, x)
+        for _ in range(2):
+            _layer(x, y, s)
+        got.append({a: s[a].clone() for a in OUT})
+    assert [t[0] for t in taken] == 2 * ["conv", "qk_norm", "scan", "conv", "scan"]
+    assert all(t[1] == B.LQ_OK for t in taken)
+    assert all(torch.equal(got[0][a], got[1][a]) for a in OUT)
+
+
+def test_irregular_calls_are_refused_by_the_python_checks():
+    n = 8
+    y = cu_args(scan_inputs(n, 2, 1, BF))
+    d = B.make_dims(1, 2, 1, rule=B.LQ_RULE_ADD)
+    cu = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    o = torch.empty((n, 2, 128), dtype=BF, device="cuda")
+    st = torch.zeros((1, 2, 128, 128), device="cuda")
+
+    def prompt(**kw):
+        a = dict(y, o=o, cu=cu, state=st, workspace=None)
+        a.update(kw)
+        B.leapquant_scan_prompt(d, a["q"], a["k"], a["v"], a["dt"], a["A"], a["o"], a["cu"], D=a["D"], state=a["state"])
+
+    prompt()
+    for kw, said in (({"q": y["q"].float()}, "q must be"), ({"o": o.half()}, "o must be"), ({"cu": cu.long()}, "cu_seqlens must be"),
+                     ({"cu": cu[:1]}, "sequences"), ({"A": y["A"].cpu()}, "device tensor"), ({"D": y["D"][:1]}, "D must have shape"),
+                     ({"state": st.transpose(2, 3)}, "state must be contiguous"), ({"dt": y["dt"].t()}, "dt must have shape"),
+                     ({"k": y["k"].transpose(1, 2)}, "k must have shape"), ({"v": y["v"][..., :64]}, "v must have shape"),
+                     ({"state": st.double()}, "state must be")):
+        with pytest.raises(ValueError, match=said):
+            prompt(**kw)
+    c = rnd(1, n, 64).cuda()
+    w = rnd(2, 64, 4).cuda()
+    B.leapquant_conv_prompt(c, w, torch.empty_like(c), cu)
+    for args, said in (((c.half(), w, torch.empty_like(c), cu), "float32 or bfloat16"), ((c, w[:32], torch.empty_like(c), cu), "weight"),
+                       ((c, w, torch.empty_like(c)[:4], cu), "out must have shape")):
+        with pytest.raises(ValueError, match=said):
+            B.leapquant_conv_prompt(*args)
+    with pytest.raises(B.LeapQuantError):
+        B.leapquant_conv_prompt(c, rnd(2, 64, 5).cuda(), torch.empty_like(c), cu)      # width 5
+    with pytest.raises(B.LeapQuantError):
+        B.leapquant_scan_step(d, st, y["q"], y["k"], y["v"], y["dt"], y["A"], o)       # 8 tokens, 1 request
