@@ -4,6 +4,8 @@
 // Bound: HBM; K multiply-adds per value read.  A thread owns 16 bytes of
 // channels of a run of tokens, whose input rows it reads once into registers;
 // neighbouring lanes own neighbouring channels, so every access is whole lines.
+#include <algorithm>
+
 #include "lq_layer.hpp"
 #include "lq_internal.hpp"
 
@@ -11,7 +13,7 @@ namespace lq {
 
 namespace {
 
-constexpr int RUN = 16;     // tokens of a wave
+constexpr int RUN = 8;      // tokens that a wave has in registers at a time
 
 struct ConvArgs {
     const char *x;
@@ -21,7 +23,7 @@ struct ConvArgs {
     const int32_t *cu, *slots;
     int32_t *err;
     int64_t tokens, x_stride, out_stride;      // strides in bytes
-    int32_t seqs, channels, n_slots, silu, carry, blocks_c, blocks_t;
+    int32_t seqs, channels, n_slots, silu, carry, blocks_c, blocks_t, runs;
 };
 
 template <int K, bool BF>
@@ -87,24 +89,36 @@ __device__ __forceinline__ int find_sequence(const int32_t *cu, int seqs, int64_
     return lo + __popcll(__ballot(at < hi && cu[at < hi ? at : 0] <= t)) - 1;
 }
 
-// A token whose window reaches the sequence's start, from memory.
+// The first K-1 tokens of a sequence, whose windows reach its start, and its new state,
+// from memory (inputs past the sequence's end do not count).
 template <int K, bool BF, bool OBF>
-__device__ __forceinline__ void emit_first(const ConvArgs &a, int64_t t, int64_t begin, int slot, int64_t c_bytes,
-                                        const float (*w)[K], const float *bias, int c) {
-    uint4 rows[K];
+__device__ __forceinline__ void begin_sequence(const ConvArgs &a, Span s, int slot, int64_t c_bytes, const float (*w)[K],
+                                            const float *bias, int c) {
+    const int64_t n = s.end - s.begin;
+    uint4 line[2 * (K - 1)], keep[K - 1];       // the old state's rows, then the first inputs
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-        const int64_t at = t - (K - 1) + j;
-        rows[j] = at >= begin ? *(const uint4 *)(a.x + at * a.x_stride + c_bytes)
-                              : old_row<K, BF>(a, slot, (int)(K - 1 + at - begin), c_bytes);
+    for (int j = 0; j < K - 1; ++j) {
+        line[j] = old_row<K, BF>(a, slot, j, c_bytes);
+        line[K - 1 + j] = *(const uint4 *)(a.x + (s.begin + (j < n ? j : 0)) * a.x_stride + c_bytes);
+        const int64_t at = n - (K - 1) + j;     // place in the sequence of the new state's row j
+        keep[j] = at >= 0 ? *(const uint4 *)(a.x + (s.begin + at) * a.x_stride + c_bytes)
+                          : old_row<K, BF>(a, slot, (int)(K - 1 + at), c_bytes);
     }
-    emit<K, BF, OBF>(a, a.out + t * a.out_stride + (int64_t)c * Tok<OBF>::BYTES, rows, w, bias);
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j)
+        if (j < n) emit<K, BF, OBF>(a, a.out + (s.begin + j) * a.out_stride + (int64_t)c * Tok<OBF>::BYTES, line + j, w, bias);
+    if (slot >= 0) {
+#pragma unroll
+        for (int j = 0; j < K - 1; ++j)
+            *(uint4 *)(a.state + ((int64_t)slot * (K - 1) + j) * a.channels * Tok<BF>::BYTES + c_bytes) = keep[j];
+    }
 }
 
-// One wave: RUN tokens of 64 lanes' channels.  The first K-1 tokens of a
-// sequence read the old state and its last K-1 replace it in place, so the wave
-// that holds a sequence's first token computes all of those K-1 tokens (also
-// past its run) and then writes the new state: nobody else reads the old one.
+// One wave: the channels of its 64 lanes, a.runs times RUN tokens one after the other,
+// the next RUN rows on their way meanwhile.  The first K-1 tokens of a sequence read the
+// old state and its last K-1 replace it in place, so the wave that holds a sequence's
+// first token computes all of those K-1 tokens (also past its own) and then writes the
+// new state: nobody else reads the old one.
 template <int K, bool BF, bool OBF>
 __global__ __launch_bounds__(256) void conv_prompt_kernel(ConvArgs a) {
     constexpr int V = Tok<BF>::V;
@@ -129,58 +143,64 @@ __global__ __launch_bounds__(256) void conv_prompt_kernel(ConvArgs a) {
         return;
     }
 
-    const int64_t t0 = ((int64_t)block * 4 + wave) * RUN;
-    if (t0 >= a.tokens) return;
-    const int64_t t1 = min(t0 + RUN, a.tokens);
-    uint4 rows[RUN + K - 1];                    // input rows t0 - (K-1) .. t0 + RUN - 1
+    const int64_t first = ((int64_t)block * 4 + wave) * (RUN * a.runs);
+    if (first >= a.tokens) return;
+    const int64_t last = min(first + RUN * a.runs, a.tokens);
+    const char *xc = a.x + cb;
+    uint4 rows[K - 1 + RUN], next[RUN];         // input rows t0 - (K-1) .. t0 + RUN - 1, and the RUN after them
 #pragma unroll
-    for (int i = 0; i < RUN + K - 1; ++i) {
-        const int64_t t = min(max(t0 - (K - 1) + i, (int64_t)0), a.tokens - 1);
-        rows[i] = *(const uint4 *)(a.x + t * a.x_stride + cb);
+    for (int i = 0; i < K - 1 + RUN; ++i) {
+        const int64_t t = min(max(first - (K - 1) + i, (int64_t)0), a.tokens - 1);
+        rows[i] = *(const uint4 *)(xc + t * a.x_stride);
     }
     float w[V][K], bias[V];
     load_params<K, BF>(a, here ? c : 0, w, bias);
 
-    int b = find_sequence(a.cu, a.seqs, t0, lane);
+    const int first_b = find_sequence(a.cu, a.seqs, first, lane);
+    int b = first_b;
     Span s{0, 0};
-    int64_t next = a.tokens;                    // the next sequence's first token
+    int64_t following = a.tokens;               // the next sequence's first token
     auto enter = [&]() {
         if (b >= 0) s = sequence_span(a.cu, b, a.tokens);
-        next = b + 1 < a.seqs ? (int64_t)a.cu[b + 1] : a.tokens;
+        following = b + 1 < a.seqs ? (int64_t)a.cu[b + 1] : a.tokens;
     };
     enter();
+    for (int64_t t0 = first; t0 < last; t0 += RUN) {
+        if (t0 + RUN < last) {
 #pragma unroll
-    for (int i = 0; i < RUN; ++i) {
-        const int64_t t = t0 + i;
-        if (t >= t1) break;
-        while (t >= next && b + 1 < a.seqs) {
-            ++b;
-            enter();
+            for (int i = 0; i < RUN; ++i) next[i] = *(const uint4 *)(xc + min(t0 + RUN + i, a.tokens - 1) * a.x_stride);
         }
-        if (b < 0 || t >= s.end || t < s.begin) continue;      // belongs to no sequence
-        const int64_t pos = t - s.begin;
-        if (pos >= K - 1) {
-            if (here) emit<K, BF, OBF>(a, a.out + t * a.out_stride + (int64_t)c * Tok<OBF>::BYTES, rows + i, w, bias);
-        } else if (pos == 0) {
-            const int slot = state_row(a.state, a.slots, b, a.n_slots, a.err);
+        char *to = a.out + t0 * a.out_stride + (int64_t)c * Tok<OBF>::BYTES;
+        if (b >= 0 && t0 - s.begin >= K - 1 && t0 + RUN <= s.end) {
+            // all of it inside one sequence, past its start
             if (here) {
-                const int64_t n = s.end - s.begin;
-                for (int j = 0; j < K - 1 && j < n; ++j)
-                    emit_first<K, BF, OBF>(a, t + j, s.begin, slot, cb, w, bias, c);
-                if (slot >= 0) {
-                    uint4 keep[K - 1];
 #pragma unroll
-                    for (int j = 0; j < K - 1; ++j) {
-                        const int64_t at = n - (K - 1) + j;    // place in the sequence
-                        keep[j] = at >= 0 ? *(const uint4 *)(a.x + (s.begin + at) * a.x_stride + cb)
-                                          : old_row<K, BF>(a, slot, (int)(K - 1 + at), cb);
-                    }
+                for (int i = 0; i < RUN; ++i) emit<K, BF, OBF>(a, to + i * a.out_stride, rows + i, w, bias);
+            }
+        } else {
 #pragma unroll
-                    for (int j = 0; j < K - 1; ++j)
-                        *(uint4 *)(a.state + ((int64_t)slot * (K - 1) + j) * a.channels * Tok<BF>::BYTES + cb) = keep[j];
+            for (int i = 0; i < RUN; ++i) {
+                const int64_t t = t0 + i;
+                if (t >= last) break;
+                while (t >= following && b + 1 < a.seqs) {
+                    ++b;
+                    enter();
                 }
+                if (b < 0 || t >= s.end || t < s.begin) continue;      // belongs to no sequence
+                if (t - s.begin >= K - 1 && here) emit<K, BF, OBF>(a, to + i * a.out_stride, rows + i, w, bias);
             }
         }
+#pragma unroll
+        for (int i = 0; i < K - 1; ++i) rows[i] = rows[RUN + i];
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) rows[K - 1 + i] = next[i];
+    }
+    // the sequences that begin here
+    for (b = max(first_b, 0); b < a.seqs && a.cu[b] < last; ++b) {
+        s = sequence_span(a.cu, b, a.tokens);
+        if (s.begin < first || s.begin == s.end) continue;
+        const int slot = state_row(a.state, a.slots, b, a.n_slots, a.err);
+        if (here) begin_sequence<K, BF, OBF>(a, s, slot, cb, w, bias, c);
     }
 }
 
@@ -224,6 +244,8 @@ ConvArgs conv_args(const lq_conv &c) {
     a.n_slots = c.n_slots;
     a.silu = c.silu;
     a.carry = c.carry;
+    a.runs = 1;
+    a.blocks_c = a.blocks_t = 0;
     return a;
 }
 
@@ -235,7 +257,15 @@ hipError_t launch(ConvArgs a, bool step, hipStream_t st) {
         a.carry = 1;
         hipLaunchKernelGGL((conv_step_kernel<K, BF, OBF>), dim3(a.blocks_c * a.seqs), dim3(256), 0, st, a);
     } else {
-        a.blocks_t = (int)((a.tokens + 4 * RUN - 1) / (4 * RUN));
+        // Runs per wave: as few as leave one round of workgroups (512: their registers allow
+        // two per CU), up to eight; a launch of several rounds anyway takes two.  Measured:
+        // 131 tokens x 1536 fp32 channels 6.3 us with one, 14.4 with eight; 8192 x 8192 bf16
+        // 71, 66, 69, 63, 75 us with 1, 2, 4, 8, 16 (eight: exactly one round); 32768 x
+        // 12288 bf16 306 us with two, 310 with eight.
+        const int64_t groups = (a.tokens + 4 * RUN - 1) / (4 * RUN), round = std::max(512 / a.blocks_c, 1);
+        const int64_t runs = std::max<int64_t>((groups + round - 1) / round, 1);
+        a.runs = runs > 8 ? 2 : (int)runs;
+        a.blocks_t = (int)((a.tokens + 4 * RUN * a.runs - 1) / (4 * RUN * a.runs));
         const int extra = a.state && !a.carry ? (a.seqs + 3) / 4 : 0;
         if (a.blocks_t + extra == 0) return hipSuccess;
         hipLaunchKernelGGL((conv_prompt_kernel<K, BF, OBF>), dim3(a.blocks_c * (a.blocks_t + extra)), dim3(256), 0, st, a);
