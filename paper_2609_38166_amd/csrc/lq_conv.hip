@@ -204,26 +204,37 @@ __global__ __launch_bounds__(256) void conv_prompt_kernel(ConvArgs a) {
     }
 }
 
-template <int K, bool BF, bool OBF>
+// R requests per thread: the channels' weights are read once for them.
+template <int K, bool BF, bool OBF, int R>
 __global__ __launch_bounds__(256) void conv_step_kernel(ConvArgs a) {
     constexpr int V = Tok<BF>::V;
-    const int b = blockIdx.x / a.blocks_c;
-    const int c = ((int)(blockIdx.x - b * a.blocks_c) * 256 + (int)threadIdx.x) * V;
+    const int first = blockIdx.x / a.blocks_c;
+    const int c = ((int)(blockIdx.x - first * a.blocks_c) * 256 + (int)threadIdx.x) * V;
     if (c >= a.channels) return;
     const int64_t cb = (int64_t)c * Tok<BF>::BYTES;
-    const int slot = state_row(a.state, a.slots, b, a.n_slots, a.err);
-    uint4 rows[K];
-    rows[K - 1] = *(const uint4 *)(a.x + (int64_t)b * a.x_stride + cb);
+    uint4 rows[R][K];
+    int slot[R];
 #pragma unroll
-    for (int i = 0; i < K - 1; ++i) rows[i] = old_row<K, BF>(a, slot, i, cb);
+    for (int r = 0; r < R; ++r) {
+        const int b = min(first * R + r, a.seqs - 1);
+        slot[r] = first * R + r < a.seqs ? state_row(a.state, a.slots, b, a.n_slots, a.err) : NO_SLOT;
+        rows[r][K - 1] = *(const uint4 *)(a.x + (int64_t)b * a.x_stride + cb);
+#pragma unroll
+        for (int i = 0; i < K - 1; ++i) rows[r][i] = old_row<K, BF>(a, slot[r], i, cb);
+    }
     float w[V][K], bias[V];
     load_params<K, BF>(a, c, w, bias);
-    if (slot >= 0) {
 #pragma unroll
-        for (int i = 0; i < K - 1; ++i)
-            *(uint4 *)(a.state + ((int64_t)slot * (K - 1) + i) * a.channels * Tok<BF>::BYTES + cb) = rows[i + 1];
+    for (int r = 0; r < R; ++r) {
+        const int b = first * R + r;
+        if (b >= a.seqs) break;
+        if (slot[r] >= 0) {
+#pragma unroll
+            for (int i = 0; i < K - 1; ++i)
+                *(uint4 *)(a.state + ((int64_t)slot[r] * (K - 1) + i) * a.channels * Tok<BF>::BYTES + cb) = rows[r][i + 1];
+        }
+        emit<K, BF, OBF>(a, a.out + (int64_t)b * a.out_stride + (int64_t)c * Tok<OBF>::BYTES, rows[r], w, bias);
     }
-    emit<K, BF, OBF>(a, a.out + (int64_t)b * a.out_stride + (int64_t)c * Tok<OBF>::BYTES, rows, w, bias);
 }
 
 ConvArgs conv_args(const lq_conv &c) {
@@ -255,7 +266,14 @@ hipError_t launch(ConvArgs a, bool step, hipStream_t st) {
     a.blocks_c = (a.channels + per - 1) / per;
     if (step) {
         a.carry = 1;
-        hipLaunchKernelGGL((conv_step_kernel<K, BF, OBF>), dim3(a.blocks_c * a.seqs), dim3(256), 0, st, a);
+        // Four requests per thread where the launch fills the GPU all the same, us a call (1, 2,
+        // 4; bf16, width 4, fp32 out): 256 x 12288 14.8, 12.4, 12.2; 128 x 12288 9.1, 8.5, 8.0;
+        // 64 x 8192 4.5, 4.9, 6.1.
+        const int64_t single = (int64_t)a.blocks_c * a.seqs;
+        if (single >= 512)
+            hipLaunchKernelGGL((conv_step_kernel<K, BF, OBF, 4>), dim3(a.blocks_c * ((a.seqs + 3) / 4)), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((conv_step_kernel<K, BF, OBF, 1>), dim3((unsigned)single), dim3(256), 0, st, a);
     } else {
         // Runs per wave: as few as leave one round of workgroups (512: their registers allow
         // two per CU), up to eight; a launch of several rounds anyway takes two.  Measured:

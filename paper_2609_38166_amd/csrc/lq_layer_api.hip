@@ -12,7 +12,8 @@ namespace {
 
 using lq::hip_status;
 
-constexpr int64_t MAX_GRID = 0x7FFFFFFF;
+// a launch's work-items are counted in 32 bits: workgroups of 256
+constexpr int64_t MAX_BLOCKS = (1 << 24) - 1;
 
 bool flag(int32_t x) { return x == 0 || x == 1; }
 bool token_type(int32_t x) { return x == LQ_TOKEN_F32 || x == LQ_TOKEN_BF16; }
@@ -39,7 +40,7 @@ int32_t check_rows(const void *p, int64_t tokens, int64_t row, int64_t stride, i
 // cu_seqlens entries, slots and positions are 32-bit.
 int32_t check_tokens(int64_t tokens) {
     if (tokens < 0) return LQ_EINVAL;
-    return tokens > MAX_GRID ? LQ_EUNSUPPORTED : LQ_OK;
+    return tokens > INT32_MAX ? LQ_EUNSUPPORTED : LQ_OK;
 }
 
 int32_t check_state(const void *state, int32_t n_slots, const int32_t *slots, int32_t seqs, bool needed) {
@@ -61,9 +62,9 @@ int32_t check_conv(const lq_conv *c, bool step) {
     if (c->width < 2 || c->width > LQ_MAX_CONV_WIDTH) return LQ_EUNSUPPORTED;
     const int32_t per = c->dtype == LQ_TOKEN_BF16 ? 8 : 4;
     if (c->channels % per) return LQ_EUNSUPPORTED;
-    // workgroups: 16 tokens and 64 lanes of channels a wave, or a state of a sequence
-    const int64_t blocks = ((int64_t)c->channels / per + 63) / 64 * ((c->tokens + 63) / 64 + c->seqs);
-    if (blocks > MAX_GRID) return LQ_EUNSUPPORTED;
+    // workgroups: at least 32 tokens of 64 lanes' channels (the step: a request), or 4 states
+    const int64_t blocks = ((int64_t)c->channels / per + 63) / 64 * ((c->tokens + 31) / 32 + c->seqs);
+    if (blocks > MAX_BLOCKS) return LQ_EUNSUPPORTED;
     if ((e = check(c->weight, 16)) != LQ_OK) return e;
     if ((e = check(c->bias, 4, false)) != LQ_OK) return e;
     if ((e = check_rows(c->x, c->tokens, c->channels, c->x_stride, token_size(c->dtype), 16)) != LQ_OK) return e;
@@ -85,7 +86,8 @@ int32_t check_scan(const lq_dims *d, const lq_scan *s, int what) {
     if ((e = check(s->A, 4)) != LQ_OK) return e;
     if ((e = check(s->dt_bias, 4, false)) != LQ_OK) return e;
     if ((e = check_rows(s->dt, T, d->heads_v, s->dt_stride, es, (uintptr_t)es)) != LQ_OK) return e;
-    if (what == 2) return T * d->heads_v > 256 * MAX_GRID ? LQ_EUNSUPPORTED : LQ_OK;
+    if (what == 2) return T * d->heads_v > 256 * MAX_BLOCKS ? LQ_EUNSUPPORTED : LQ_OK;
+    if ((int64_t)d->batch * d->heads_v > MAX_BLOCKS / 8) return LQ_EUNSUPPORTED;      // (up to eight workgroups a tile)
     if (s->state_dtype != LQ_STATE_F32 && s->state_dtype != LQ_STATE_BF16) return LQ_EINVAL;
     if (!flag(s->carry) || s->max_len < 0) return LQ_EINVAL;
     if (what == 1 && T != d->batch) return LQ_EINVAL;
@@ -130,7 +132,7 @@ int32_t leapquant_qk_norm(const lq_qk *n, void *stream) {
     if (n->d != 64 && n->d != 128 && n->d != 256) return LQ_EUNSUPPORTED;
     if (n->rot % 16 || n->rot > n->d) return LQ_EUNSUPPORTED;
     if ((int64_t)n->heads_q + n->heads_k > (1 << 20)) return LQ_EUNSUPPORTED;
-    if (n->tokens * ((int64_t)n->heads_q + n->heads_k) / (2048 / n->d) >= MAX_GRID) return LQ_EUNSUPPORTED;
+    if (n->tokens * ((int64_t)n->heads_q + n->heads_k) / (2048 / n->d) >= MAX_BLOCKS) return LQ_EUNSUPPORTED;
     const int64_t es = token_size(n->dtype), eo = token_size(n->out_dtype);
     const int64_t rq = (int64_t)n->heads_q * n->d, rk = (int64_t)n->heads_k * n->d;
     if ((e = check_rows(n->q, n->tokens, rq, n->q_stride, es, 16)) != LQ_OK) return e;

@@ -29,42 +29,44 @@ __device__ __forceinline__ void load8(const char *p, float *f) {
 
 // ---- single tokens ------------------------------------------------------------
 //
-// Bound: HBM, the state read and written once.  One workgroup per (request,
-// value head); 16 lanes hold a row of S^T (8 key channels each), so the output's
-// sum is a DPP row sum.
-template <bool BF, bool SBF>
+// Bound: HBM, the state read and written once.  M rows of S^T per thread, 8 key
+// channels each: 16 lanes hold a row, so the output's sum is a DPP row sum, and a
+// workgroup holds 16 M rows, 8 / M workgroups a tile.
+template <bool BF, bool SBF, int M>
 __global__ __launch_bounds__(NT) void scan_step_kernel(ScanArgs a) {
-    const int tid = threadIdx.x, l16 = tid & 15, r0 = tid >> 4;
-    const int b = blockIdx.x / a.heads_v, h = blockIdx.x - b * a.heads_v;
+    constexpr int PARTS = 8 / M, SB = SBF ? 2 : 4;
+    const int tid = threadIdx.x, l16 = tid & 15;
+    const int tile = blockIdx.x / PARTS, r0 = (blockIdx.x % PARTS) * 16 * M + (tid >> 4);
+    const int b = tile / a.heads_v, h = tile - b * a.heads_v;
     const int slot = state_row(a.state, a.slots, b, a.n_slots, a.err);
-    float s[8][8];
-    char *St = a.state + ((int64_t)slot * a.heads_v + h) * D * D * (SBF ? 2 : 4);
+    float s[M][8];
+    char *St = a.state + ((int64_t)slot * a.heads_v + h) * D * D * SB;
     const float fill = slot == BAD_SLOT ? nanf32() : 0.0f;
 #pragma unroll
-    for (int m = 0; m < 8; ++m) {
+    for (int m = 0; m < M; ++m) {
         if (slot >= 0) {
-            load8<SBF>(St + ((r0 + 16 * m) * D + 8 * l16) * (SBF ? 2 : 4), s[m]);
+            load8<SBF>(St + ((r0 + 16 * m) * D + 8 * l16) * SB, s[m]);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[m][j] = fill;
         }
     }
     const int64_t kc = ((int64_t)(h / a.group) * D + 8 * l16) * Tok<BF>::BYTES;
-    float k[8], q[8];
+    float k[8], q[8], v[M];
     load8<BF>(a.k + (int64_t)b * a.k_stride + kc, k);
     load8<BF>(a.q + (int64_t)b * a.q_stride + kc, q);
-    const float bias = a.bias ? a.bias[h] : 0.0f;
+#pragma unroll
+    for (int m = 0; m < M; ++m) v[m] = load_tok<BF>(a.v + (int64_t)b * a.v_stride, (int64_t)h * D + r0 + 16 * m);
+    const float bias = a.bias ? a.bias[h] : 0.0f, skip = a.skip ? a.skip[h] : 0.0f;
     const float delta = scan_delta(load_tok<BF>(a.dt + (int64_t)b * a.dt_stride, h) + bias, a.softplus);
     const float alpha = scan_alpha(delta * a.A[h]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) k[j] *= delta;
 #pragma unroll
-    for (int m = 0; m < 8; ++m) {
-        const int row = r0 + 16 * m;
-        const float v = load_tok<BF>(a.v + (int64_t)b * a.v_stride, (int64_t)h * D + row);
+    for (int m = 0; m < M; ++m) {
         float y = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[m][j] = fmaf(k[j], v, alpha * s[m][j]);
+        for (int j = 0; j < 8; ++j) s[m][j] = fmaf(k[j], v[m], alpha * s[m][j]);
         if (SBF) {                                   // the output reads the state as it is stored
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
@@ -73,18 +75,16 @@ __global__ __launch_bounds__(NT) void scan_step_kernel(ScanArgs a) {
                 s[m][j + 1] = __uint_as_float(w & 0xFFFF0000u);
             }
         }
+        if (slot >= 0) store_tok<SBF, 8>(St + ((r0 + 16 * m) * D + 8 * l16) * SB, s[m]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) y = fmaf(s[m][j], q[j], y);
-        y = row16_sum(y) + (a.skip ? a.skip[h] * v : 0.0f);
+        y = row16_sum(y);
+        if (a.skip) y = fmaf(skip, v[m], y);
         if (l16 == 0) {
             char *o = a.o + (int64_t)b * a.o_stride;
-            if (BF) ((uint16_t *)o)[h * D + row] = (uint16_t)pk_bf16(y, y);
-            else ((float *)o)[h * D + row] = y;
+            if (BF) ((uint16_t *)o)[h * D + r0 + 16 * m] = (uint16_t)pk_bf16(y, y);
+            else ((float *)o)[h * D + r0 + 16 * m] = y;
         }
-    }
-    if (slot >= 0) {
-#pragma unroll
-        for (int m = 0; m < 8; ++m) store_tok<SBF, 8>(St + ((r0 + 16 * m) * D + 8 * l16) * (SBF ? 2 : 4), s[m]);
     }
 }
 
@@ -819,6 +819,22 @@ hipError_t launch_prompt(const lq_dims &d, const lq_scan &s, hipStream_t st) {
     return hipGetLastError();
 }
 
+template <bool BF, bool SBF>
+hipError_t launch_step(const lq_dims &d, const lq_scan &s, hipStream_t st) {
+    const ScanArgs a = scan_args(d, s);
+    const int tiles = d.batch * d.heads_v;
+    // Rows per thread, us a call (1, 2, 4, 8): fp32 8192 tiles 185, 201, 203, 212; 2048 51, 52,
+    // 54, 59; 512 14.8, 13.4, 13.8, 14.0; bf16 8192 123, 101, 104, 115; 16 4.2, 4.2, 4.6, 5.0.
+    if constexpr (!SBF) {
+        if (tiles >= 2048) {
+            hipLaunchKernelGGL((scan_step_kernel<BF, SBF, 1>), dim3(8 * tiles), dim3(NT), 0, st, a);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((scan_step_kernel<BF, SBF, 2>), dim3(4 * tiles), dim3(NT), 0, st, a);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t scan_workspace_bytes(const lq_dims &d, const lq_scan &s) { return split_of(d, s).bytes; }
@@ -828,17 +844,9 @@ hipError_t launch_scan_prompt(const lq_dims &d, const lq_scan &s, hipStream_t st
 }
 
 hipError_t launch_scan_step(const lq_dims &d, const lq_scan &s, hipStream_t st) {
-    const ScanArgs a = scan_args(d, s);
-    const dim3 grid(d.batch * d.heads_v);
     const bool sbf = s.state_dtype == LQ_STATE_BF16;
-    if (s.dtype == LQ_TOKEN_BF16) {
-        if (sbf) hipLaunchKernelGGL((scan_step_kernel<true, true>), grid, dim3(NT), 0, st, a);
-        else hipLaunchKernelGGL((scan_step_kernel<true, false>), grid, dim3(NT), 0, st, a);
-    } else {
-        if (sbf) hipLaunchKernelGGL((scan_step_kernel<false, true>), grid, dim3(NT), 0, st, a);
-        else hipLaunchKernelGGL((scan_step_kernel<false, false>), grid, dim3(NT), 0, st, a);
-    }
-    return hipGetLastError();
+    if (s.dtype == LQ_TOKEN_BF16) return sbf ? launch_step<true, true>(d, s, st) : launch_step<true, false>(d, s, st);
+    return sbf ? launch_step<false, true>(d, s, st) : launch_step<false, false>(d, s, st);
 }
 
 hipError_t launch_scan_gates(const lq_dims &d, const lq_scan &s, float *alpha, float *beta, hipStream_t st) {

@@ -540,3 +540,33 @@ def test_irregular_calls_are_refused_by_the_python_checks():
         B.leapquant_conv_prompt(c, rnd(2, 64, 5).cuda(), torch.empty_like(c), cu)      # width 5
     with pytest.raises(B.LeapQuantError):
         B.leapquant_scan_step(d, st, y["q"], y["k"], y["v"], y["dt"], y["A"], o)       # 8 tokens, 1 request
+
+
+@pytest.mark.parametrize("batch,c", [(513, 64), (1026, 2056)])
+def test_conv_step_of_many_requests(batch, c):
+    """Several requests per thread, a last group of fewer."""
+    x, w, b, state = rnd(1, batch, c).to(BF), rnd(2, c, 4), rnd(3, c), rnd(4, batch, 3, c).to(BF)
+    st = state.cuda()
+    o = torch.empty((batch, c), device="cuda")
+    B.leapquant_conv_step(x.cuda(), w.cuda(), o, st, bias=b.cuda())
+    line = torch.cat([state, x[:, None]], 1).double()
+    m = (line * w.t().double()).abs().sum(1) + b.double().abs()
+    y = (line * w.t().double()).sum(1) + b.double()
+    close(o, y / (1 + torch.exp(-y)), 1e-6 * (m + 1))
+    assert torch.equal(st.cpu(), line[:, 1:].to(BF))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_scan_step_of_many_tiles(dtype):
+    """Enough tiles that a row of the state is a thread's whole share."""
+    batch, hv = 128, 17
+    x = scan_inputs(batch, hv, 1, dtype)
+    state = rnd(9, batch, hv, 128, 128)
+    want, osize, new, size = R.scan(x["q"], x["k"], x["v"], x["dt"], x["A"], [(b, b + 1) for b in range(batch)], x["D"],
+                                    x["dt_bias"], True, state)
+    st, y = state.cuda(), cu_args(x)
+    o = torch.empty((batch, hv, 128), dtype=dtype, device="cuda")
+    B.leapquant_scan_step(B.make_dims(batch, hv, 1, rule=B.LQ_RULE_ADD), st, y["q"], y["k"], y["v"], y["dt"], y["A"], o,
+                          D=y["D"], dt_bias=y["dt_bias"])
+    close(o, want, (128 + 24) * U * osize)
+    close(st, new, 24 * U * size)
