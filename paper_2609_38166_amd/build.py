@@ -38,10 +38,12 @@ FLAGS = [
 #    positions (2.2% on the GQA GDN layer), no spill;
 #  - tile kernel: the AMDGPU register-pressure trackers, for the scalar gate's
 #    exports, which spill without them: 8192 E4M3 states with 33 records 291 us
-#    instead of 255 (2048: 76 and 73); commits and quantizations within 1%.
+#    instead of 255 (2048: 76 and 73); commits and quantizations within 1%;
+#  - scan: max-ILP, 2048 fp32 tokens x 32 heads 124 -> 107 us; bf16 prompts within 2%.
 SCHED = {
     "lq_decode.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"],
     "lq_tile.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers"],
+    "lq_scan.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"],
 }
 
 

@@ -1,6 +1,7 @@
 // Selective state space scan, packed prompts and single tokens:
 //   S_t = alpha_t S_{t-1} + delta_t k_t v_t^T,   o_t = S_t^T q_t + skip v_t,
 // delta = softplus(dt + bias), alpha = exp(delta A), the state kept as S^T.
+#include <algorithm>
 #include <type_traits>
 
 #include "lq_layer.hpp"
@@ -155,7 +156,16 @@ template <bool BF> struct Chunk {
     __device__ static __forceinline__ int place(int row, int piece) {
         return piece ^ (BF ? 4 * (row & 3) + ((row >> 2) & 3) : row & 15);
     }
-    __device__ static __forceinline__ int at(int row, int piece) { return row * ROW + (place(row, piece) << 4); }
+    // Offsets in an array's rows from which the products' operands follow by an exclusive
+    // or: of piece g of row l16 (piece 4 s + g: s << 6), and, where a product sums over
+    // tokens, of this lane's first columns of its first row (bf16 row 4 g + (l16 >> 2),
+    // tile i: (i >> 1) << 6, and 8 for an odd i on top; fp32 row 4 g, row r and tile i:
+    // r << 4 | i << 6, and r rows on top).
+    __device__ static __forceinline__ int row_operand(int l16, int g) { return l16 * ROW + (place(l16, g) << 4); }
+    __device__ static __forceinline__ int token_operand(int l16, int g) {
+        return BF ? (4 * g + (l16 >> 2)) * ROW + (place(4 * g + (l16 >> 2), l16 & 3) << 4)
+                  : 4 * g * ROW + (place(4 * g, l16 >> 2) << 4) + 4 * (l16 & 3);
+    }
     // Key channel of register 0 of state tile i (0..7) in lane group g, and value
     // channel of a lane in tile u of its wave: bf16 deals rows so that tiles 2i and
     // 2i+1 hold 8 neighbouring key channels, and u = 0, 1 8 neighbouring outputs.
@@ -196,13 +206,23 @@ __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
+// LDS by its byte address.
+template <typename T>
+__device__ __forceinline__ T lds_read(uint32_t at) { return *(const __attribute__((address_space(3))) T *)(uintptr_t)at; }
+
+__device__ __forceinline__ uint4 lds_read16(uint32_t at) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(uint4, lds_read<u32x4>(at));
+}
+
 // 8 rows x 16 columns of bf16 in LDS turned: the lanes of a 16-lane group pass the
-// addresses of rows l16 >> 2 (p) and 4 + (l16 >> 2) (p2), 4 columns each, and a lane
-// receives its column (4 columns of lane l16 >> 2's, number l16 & 3) of the 8 rows.
-__device__ __forceinline__ bf16x8 frag_turned(const char *p, const char *p2) {
+// address of row l16 >> 2 of the first 4 rows, 4 columns each (the other 4 rows lie 16
+// rows on), and a lane receives its column (number l16 & 3 of the 4 of lane l16 >> 2) of
+// the 8 rows.
+__device__ __forceinline__ bf16x8 frag_turned(uint32_t at) {
     typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p2);
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)at);
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)(at + 16 * 256));
     const s16x8 r = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     return __builtin_bit_cast(bf16x8, r);
 }
@@ -272,12 +292,11 @@ __device__ __forceinline__ void find_segment(const ScanArgs &a, int seg, int len
 }
 
 template <bool BF, int MODE>
-__global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
+__global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
     using K = Chunk<BF>;
     constexpr int C = K::C, TILES = K::TILES;
     constexpr int ARRAYS = MODE == PARTS ? 2 : 3;           // keys, values, queries
-    constexpr int AHEAD = 2;                                // chunks on their way
-    __shared__ __attribute__((aligned(16))) char rows[AHEAD + 1][ARRAYS][K::BYTES];
+    __shared__ __attribute__((aligned(16))) char rows[2][ARRAYS][K::BYTES];
     __shared__ uint32_t steps[K::GROUP * C];                // dt of a group as it lies in memory
     __shared__ typename K::Rates rates[2][K::GROUP];
     const ScanArgs &a = p.s;
@@ -311,10 +330,10 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
     }
 
     // The rows of a chunk on their way into LDS, 2 KiB of each array per wave in two
-    // copies: lane by lane the pieces that belong at the lane's place.  The second
-    // copy's rows lie SECOND rows on, their pieces `turned` bytes aside.
-    constexpr int SECOND = 64 / K::PIECES;
-    const int row0 = 64 * 2 * wave / K::PIECES + lane / K::PIECES;
+    // copies: lane by lane the pieces that belong at the lane's place.  The second copy's
+    // rows lie half a chunk on, their pieces `turned` bytes aside (bf16: the same pieces).
+    constexpr int SECOND = C / 2;
+    const int row0 = (64 * wave + lane) / K::PIECES;
     const int turned = 16 * (K::place(row0 + SECOND, lane % K::PIECES) - K::place(row0, lane % K::PIECES));
     const int64_t stride[3] = {a.k_stride, a.v_stride, a.q_stride};
     const char *from[ARRAYS];
@@ -327,16 +346,16 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
     auto copy_chunk = [&](int buf, int left) {            // left: tokens of the segment from this chunk on
 #pragma unroll
         for (int n = 0; n < ARRAYS; ++n) {
-            char *to = rows[buf][n] + 2048 * wave;
+            char *to = rows[buf][n] + 1024 * wave;
             if (left >= C) {
                 dma16(from[n], lds_addr(to));
-                dma16(from[n] + SECOND * stride[n] + turned, lds_addr(to + 1024));
+                dma16(from[n] + SECOND * stride[n] + turned, lds_addr(to + K::BYTES / 2));
             } else {
                 // past the segment's end lie other tokens, or none: zeros stand in for them
                 if (row0 < left) dma16(from[n], lds_addr(to));
                 else *(uint4 *)(to + 16 * lane) = make_uint4(0u, 0u, 0u, 0u);
-                if (row0 + SECOND < left) dma16(from[n] + SECOND * stride[n] + turned, lds_addr(to + 1024));
-                else *(uint4 *)(to + 1024 + 16 * lane) = make_uint4(0u, 0u, 0u, 0u);
+                if (row0 + SECOND < left) dma16(from[n] + SECOND * stride[n] + turned, lds_addr(to + K::BYTES / 2));
+                else *(uint4 *)(to + K::BYTES / 2 + 16 * lane) = make_uint4(0u, 0u, 0u, 0u);
             }
             from[n] += C * stride[n];
         }
@@ -369,9 +388,7 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
 
     if (begin < end) {
         if (turn_of(0)) copy_steps(begin);
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (begin + i * C < end) copy_chunk(i, (int)(end - begin) - i * C);
+        copy_chunk(0, (int)(end - begin));
     }
 
     // the state: tile [i][u], registers = 4 key channels
@@ -400,89 +417,30 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
         put_rates(0, begin);
     }
     double total = 0.0;                                   // log2 decay of the segment
-    int chunk = 0, buf = 0;
+    int chunk = 0;
     for (int64_t t0 = begin; t0 < end; t0 += C, ++chunk) {
-        // This chunk's rows have arrived, and nobody reads the last one's any more.  Younger
-        // than its copies are the next chunk's, if that is a whole one (a wave skips copies
-        // past the segment's end), and the last chunk's output stores.
-        constexpr int COPIES = 2 * ARRAYS, STORES = MODE == PARTS ? 0 : 2;
-        if (t0 + 2 * C > end) wait_vm_all();
-        else if (chunk == 0) wait_vm<COPIES>();
-        else wait_vm<COPIES + STORES>();
+        // this chunk's rows have arrived, and nobody reads the last one's any more
+        wait_vm_all();
         __syncthreads();
-        const int group = chunk / K::GROUP;
-        const char *kr = rows[buf][0], *vr = rows[buf][1], *qr = rows[buf][ARRAYS - 1];
+        const int buf = chunk & 1, group = chunk / K::GROUP;
         const typename K::Rates &rate = rates[group & 1][chunk % K::GROUP];
-        buf = buf == AHEAD ? 0 : buf + 1;                 // the next chunk's; the one after it goes where the last one was
-        // the next group: its steps set out with this one's first chunk and are there (older
-        // than the rows of its third, which were waited for) when that begins
+        // the next group: its steps set out with this one's first chunk and are there before its third
         if (turn_of(group + 1)) {
             if (chunk % K::GROUP == 0) copy_steps(t0 + GROUP_TOKENS);
             if (chunk % K::GROUP == 2) put_rates(group + 1, t0 + GROUP_TOKENS - 2 * C);
         }
-        if (t0 + AHEAD * C < end) copy_chunk(buf == AHEAD ? 0 : buf + 1, (int)(end - t0) - AHEAD * C);
+        if (t0 + C < end) copy_chunk(buf ^ 1, (int)(end - t0) - C);
 
-        // LDS reads set out well ahead of their use (pin() keeps them there; arithmetic may
-        // cross it): left to the compiler they stood right before it, some 20 round trips
-        // a chunk in the open.
-        auto pin = [] { __builtin_amdgcn_sched_barrier(1); };
+        // LDS addresses of the operands.  The empty asm keeps the compiler from holding the
+        // dozens that follow from these two in registers of their own across the loop.
+        uint32_t by_row = lds_addr(rows[buf][0]) + K::row_operand(l16, g);
+        uint32_t by_token = lds_addr(rows[buf][0]) + K::token_operand(l16, g);
+        asm volatile("" : "+v"(by_row), "+v"(by_token));
+        constexpr uint32_t VALUES = K::BYTES, QUERIES = 2 * K::BYTES;
+        typedef typename K::Operand Operand;
 
-        // Values as operands that sum over tokens, dealt like P's tiles: slots 4 J + r of
-        // lane group g are the tokens 16 J + 4 g + r.
-        bf16x8 xb[2];
-        float xf[2][4];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if constexpr (BF) {
-                const int row = 4 * g + (l16 >> 2), piece = 4 * wave + (l16 & 3);
-                xb[u] = frag_turned(vr + K::at(row, piece) + 8 * u, vr + K::at(row + 16, piece) + 8 * u);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    xf[u][r] = *(const float *)(vr + K::at(4 * g + r, 8 * wave + 4 * u + (l16 >> 2)) + 4 * (l16 & 3));
-            }
-        }
-        f32x4 w[TILES];
-#pragma unroll
-        for (int J = 0; J < TILES; ++J) w[J] = *(const f32x4 *)(rate.w + 16 * J + 4 * g);
-        const double g_end = rate.g[C - 1];
-
-        f32x4 y[TILES][2], sc[TILES][TILES], weight[TILES][TILES];
-        float grown[TILES];
-        bool odd = false;                       // a value that is not finite
+        f32x4 y[TILES][2], sc[TILES][TILES];
         if (MODE != PARTS) {
-            // operands of step s of the products below: keys and queries of its channels
-            typedef typename K::Operand Operand;
-            Operand kf[2][TILES], qf[2][TILES];
-            auto load_kq = [&](int s) {
-#pragma unroll
-                for (int T = 0; T < TILES; ++T) {
-                    kf[s & 1][T] = *(const Operand *)(kr + K::at(16 * T + l16, 4 * s + g));
-                    qf[s & 1][T] = *(const Operand *)(qr + K::at(16 * T + l16, 4 * s + g));
-                }
-            };
-            double gt[TILES], gj[TILES][4];
-            f32x4 dl[TILES];
-#pragma unroll
-            for (int T = 0; T < TILES; ++T) {
-                gt[T] = rate.g[16 * T + l16];
-                dl[T] = *(const f32x4 *)(rate.delta + 16 * T + 4 * g);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) gj[T][r] = rate.g[16 * T + 4 * g + r];
-            }
-            load_kq(0);
-            pin();
-
-            // P's weights and 2^G_t
-#pragma unroll
-            for (int T = 0; T < TILES; ++T) {
-                grown[T] = exp2_hw((float)gt[T]);
-#pragma unroll
-                for (int J = 0; J <= T; ++J)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) weight[J][T][r] = exp2_hw((float)(gt[T] - gj[J][r])) * dl[J][r];
-            }
-
             // P^T's tiles (rows of keys J, columns of queries T, J <= T) and, from the same
             // queries, what the state gives: y^T = S^T q^T
 #pragma unroll
@@ -491,16 +449,19 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
 #pragma unroll
                 for (int J = 0; J < TILES; ++J) sc[J][T] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             }
-            constexpr int STEPS = BF ? 4 : 8;
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                if (s + 1 < STEPS) load_kq(s + 1);
-                pin();
+            for (int s = 0; s < (BF ? 4 : 8); ++s) {
+                Operand kf[TILES], qf[TILES];
+#pragma unroll
+                for (int T = 0; T < TILES; ++T) {
+                    kf[T] = lds_read<Operand>((by_row ^ (s << 6)) + 16 * T * K::ROW);
+                    qf[T] = lds_read<Operand>((by_row ^ (s << 6)) + 16 * T * K::ROW + QUERIES);
+                }
                 if constexpr (BF) {
 #pragma unroll
                     for (int T = 0; T < TILES; ++T)
 #pragma unroll
-                        for (int J = 0; J <= T; ++J) sc[J][T] = mfma(kf[s & 1][J], qf[s & 1][T], sc[J][T]);
+                        for (int J = 0; J <= T; ++J) sc[J][T] = mfma(kf[J], qf[T], sc[J][T]);
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         float x[8];
@@ -508,63 +469,63 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
                         for (int e = 0; e < 8; ++e) x[e] = S[2 * s + (e >> 2)][u][e & 3];
                         const bf16x8 hi = split8(x), lo = pack8(x);
 #pragma unroll
-                        for (int T = 0; T < TILES; ++T) y[T][u] = mfma(hi, qf[s & 1][T], y[T][u]);
+                        for (int T = 0; T < TILES; ++T) y[T][u] = mfma(hi, qf[T], y[T][u]);
 #pragma unroll
-                        for (int T = 0; T < TILES; ++T) y[T][u] = mfma(lo, qf[s & 1][T], y[T][u]);
+                        for (int T = 0; T < TILES; ++T) y[T][u] = mfma(lo, qf[T], y[T][u]);
                     }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        sc[0][0] = mfma(kf[s & 1][0][e], qf[s & 1][0][e], sc[0][0]);
-                        y[0][0] = mfma(S[s][0][e], qf[s & 1][0][e], y[0][0]);
-                        y[0][1] = mfma(S[s][1][e], qf[s & 1][0][e], y[0][1]);
+                        sc[0][0] = mfma(kf[0][e], qf[0][e], sc[0][0]);
+                        y[0][0] = mfma(S[s][0][e], qf[0][e], y[0][0]);
+                        y[0][1] = mfma(S[s][1][e], qf[0][e], y[0][1]);
+                    }
+                }
+            }
+            // 2^G_t on what the state gives, P's weights on the tiles
+#pragma unroll
+            for (int T = 0; T < TILES; ++T) {
+                const double gt = rate.g[16 * T + l16];
+                const float grown = exp2_hw((float)gt);
+                y[T][0] *= grown;
+                y[T][1] *= grown;
+#pragma unroll
+                for (int J = 0; J <= T; ++J) {
+                    const int j0 = 16 * J + 4 * g;
+                    const f32x4 dl = *(const f32x4 *)(rate.delta + j0);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float x = sc[J][T][r] * (exp2_hw((float)(gt - rate.g[j0 + r])) * dl[r]);
+                        sc[J][T][r] = J < T || 4 * g + r <= l16 ? x : 0.0f;
                     }
                 }
             }
         }
 
-        // keys as operands that sum over tokens, for the state
-        bf16x8 kb[8];
-        float kt[4][8];
-        if constexpr (BF) {
+        // Values as operands that sum over tokens, dealt like P's tiles: slots 4 J + r of
+        // lane group g are the tokens 16 J + 4 g + r.
+        bf16x8 xb[2];
+        float xf[2][4];
+        bool odd = false;                       // a value that is not finite
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int row = 4 * g + (l16 >> 2), piece = 4 * (i >> 1) + (l16 & 3);
-                kb[i] = frag_turned(kr + K::at(row, piece) + 8 * (i & 1), kr + K::at(row + 16, piece) + 8 * (i & 1));
-            }
-        } else {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    kt[r][i] = *(const float *)(kr + K::at(4 * g + r, 4 * i + (l16 >> 2)) + 4 * (l16 & 3));
-        }
-        pin();
-
-        if (MODE != PARTS) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if constexpr (BF) {
+        for (int u = 0; u < 2; ++u) {
+            if constexpr (BF) {
+                xb[u] = frag_turned((by_token ^ (wave << 6)) + VALUES + 8 * u);
+                if (MODE != PARTS) {
                     const uint4 v = __builtin_bit_cast(uint4, xb[u]);
                     const uint32_t m = 0x7F807F80u, c = 0x00800080u;
                     odd |= ((((v.x & m) + c) | ((v.y & m) + c) | ((v.z & m) + c) | ((v.w & m) + c)) & 0x80008000u) != 0;
-                } else {
+                }
+            } else {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) odd |= (__float_as_uint(xf[u][r]) & 0x7F800000u) == 0x7F800000u;
+                for (int r = 0; r < 4; ++r) {
+                    xf[u][r] = lds_read<float>((by_token ^ (r << 4 | (2 * wave + u) << 6)) + r * K::ROW + VALUES);
+                    if (MODE != PARTS) odd |= (__float_as_uint(xf[u][r]) & 0x7F800000u) == 0x7F800000u;
                 }
             }
-#pragma unroll
-            for (int T = 0; T < TILES; ++T) {
-                y[T][0] *= grown[T];
-                y[T][1] *= grown[T];
-#pragma unroll
-                for (int J = 0; J <= T; ++J)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float x = sc[J][T][r] * weight[J][T][r];
-                        sc[J][T][r] = J < T || 4 * g + r <= l16 ? x : 0.0f;
-                    }
-            }
+        }
+
+        if (MODE != PARTS) {
             if (!__any(odd)) {
                 if constexpr (BF) {
 #pragma unroll
@@ -574,10 +535,9 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
                         for (int e = 0; e < 8; ++e) x[e] = (e >> 2) <= T ? sc[e >> 2][T][e & 3] : 0.0f;
                         const bf16x8 hi = split8(x), lo = pack8(x);
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            y[T][u] = mfma(xb[u], hi, y[T][u]);
-                            y[T][u] = mfma(xb[u], lo, y[T][u]);
-                        }
+                        for (int u = 0; u < 2; ++u) y[T][u] = mfma(xb[u], hi, y[T][u]);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) y[T][u] = mfma(xb[u], lo, y[T][u]);
                     }
                 } else {
 #pragma unroll
@@ -605,7 +565,8 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
 #pragma unroll
                                     for (int e = 0; e < 4; ++e) {
                                         const int c = K::out_channel(wave, u, g) + e;
-                                        const float x = load_tok<BF>(vr + K::at(j, c / Tok<BF>::V), c % Tok<BF>::V);
+                                        const char *row = rows[buf][1] + j * K::ROW + (K::place(j, c / Tok<BF>::V) << 4);
+                                        const float x = load_tok<BF>(row, c % Tok<BF>::V);
                                         if (j <= 16 * T + l16) y[T][u][e] = fmaf(pj, x, y[T][u][e]);
                                     }
                             }
@@ -619,10 +580,10 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
                 if (has_skip) {
                     float x[8];
                     if constexpr (BF) {
-                        unpack16<true>(*(const uint4 *)(vr + K::at(t, 4 * wave + g)), x);
+                        unpack16<true>(lds_read16((by_row ^ (wave << 6)) + 16 * T * K::ROW + VALUES), x);
                     } else {
-                        unpack16<false>(*(const uint4 *)(vr + K::at(t, 8 * wave + g)), x);
-                        unpack16<false>(*(const uint4 *)(vr + K::at(t, 8 * wave + 4 + g)), x + 4);
+                        unpack16<false>(lds_read16((by_row ^ (2 * wave << 6)) + VALUES), x);
+                        unpack16<false>(lds_read16((by_row ^ ((2 * wave + 1) << 6)) + VALUES), x + 4);
                     }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) out[e] = fmaf(skip, x[e], out[e]);
@@ -641,6 +602,7 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
 
         // the state moves on
         if (MODE != OUTPUT || t0 + C < end) {
+            const double g_end = rate.g[C - 1];
             const float keep = exp2_hw((float)g_end);
             if (MODE == PARTS) total += g_end;
 #pragma unroll
@@ -655,26 +617,34 @@ __global__ __launch_bounds__(256, 2) void scan_prompt_kernel(PromptArgs p) {
                     float x[8];
                     unpack16<true>(__builtin_bit_cast(uint4, xb[u]), x);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] *= w[e >> 2][e & 3];
+                    for (int J = 0; J < 2; ++J) {
+                        const f32x4 w = *(const f32x4 *)(rate.w + 16 * J + 4 * g);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) x[4 * J + r] *= w[r];
+                    }
                     wx[u][0] = split8(x);
                     wx[u][1] = split8(x);
                     wx[u][2] = pack8(x);
                 }
 #pragma unroll
-                for (int term = 0; term < 3; ++term)
+                for (int i = 0; i < 8; ++i) {
+                    const bf16x8 kf = frag_turned((by_token ^ ((i >> 1) << 6)) + 8 * (i & 1));
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        S[i][0] = mfma(kb[i], wx[0][term], S[i][0]);
-                        S[i][1] = mfma(kb[i], wx[1][term], S[i][1]);
+                    for (int term = 0; term < 3; ++term) {
+                        S[i][0] = mfma(kf, wx[0][term], S[i][0]);
+                        S[i][1] = mfma(kf, wx[1][term], S[i][1]);
                     }
+                }
             } else {
+                const f32x4 w = *(const f32x4 *)(rate.w + 4 * g);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float x0 = xf[0][r] * w[0][r], x1 = xf[1][r] * w[0][r];
+                    const float x0 = xf[0][r] * w[r], x1 = xf[1][r] * w[r];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        S[i][0] = mfma(kt[r][i], x0, S[i][0]);
-                        S[i][1] = mfma(kt[r][i], x1, S[i][1]);
+                        const float kf = lds_read<float>((by_token ^ (r << 4 | i << 6)) + r * K::ROW);
+                        S[i][0] = mfma(kf, x0, S[i][0]);
+                        S[i][1] = mfma(kf, x1, S[i][1]);
                     }
                 }
             }
@@ -769,25 +739,28 @@ ScanArgs scan_args(const lq_dims &d, const lq_scan &s) {
     return a;
 }
 
-// How a prompt's work is split.  A sequence's chunks follow one another, so a
-// launch has one workgroup per (sequence, head) unless the sequences are cut
-// into segments, which costs a second pass over keys and values and the
-// segments' states (64 KiB each, written, joined and read).
+// How a prompt's work is split.  A sequence's chunks follow one another (2.4 us a chunk of
+// 32 bf16 or 3.6 us of 16 fp32 tokens where a CU has one workgroup), so a launch has one
+// workgroup per (sequence, head) unless the sequences are cut into segments, which costs a
+// second pass over keys and values and the segments' states (64 KiB each, written, joined
+// and read).  They are cut so that the launch has two workgroups per CU, and only where a
+// segment is a small part of the longest sequence.  us without -> with, heads x tokens:
+// bf16 16 x 512 43 -> 29, 16 x 320 29 -> 25, 16 x 256 (64 a segment) 24 -> 24, of four
+// sequences 25 -> 31, 32 x 8192 566 -> 123; fp32 32 x 512 114 -> 50, 16 x 224 53 -> 38.
+// Three workgroups' worth instead of two: 32 x 8192 132, 16 x 32768 237 instead of 232;
+// one: 141, 268.
 struct Split {
-    int32_t length;         // 0: not cut
+    int32_t length;         // tokens of a segment; 0: not cut
     int64_t segments;
     size_t bytes;
 };
 Split split_of(const lq_dims &d, const lq_scan &s) {
-    constexpr int64_t FULL = 512;               // two workgroups on each of the 256 CUs
-    constexpr int64_t LEAST = 256;              // tokens that a segment is worth
+    constexpr int64_t FULL = 512;               // workgroups
     Split r{0, d.batch, 0};
     const int64_t longest = s.max_len > 0 && s.max_len < s.tokens ? s.max_len : s.tokens;
-    const int64_t units = (int64_t)d.batch * d.heads_v;
-    if (units >= FULL || longest <= 2 * LEAST) return r;
-    int64_t length = (s.tokens * d.heads_v / FULL + 63) / 64 * 64;
-    if (length < LEAST) length = LEAST;
-    if (length >= longest) return r;
+    if ((int64_t)d.batch * d.heads_v >= FULL) return r;
+    const int64_t length = std::max<int64_t>((s.tokens * d.heads_v / FULL + 63) / 64 * 64, 64);
+    if (longest <= (s.dtype == LQ_TOKEN_BF16 ? 4 : 3) * length) return r;
     r.length = (int32_t)length;
     r.segments = s.tokens / length + d.batch;   // each sequence's last segment may be short
     r.bytes = (size_t)r.segments * d.heads_v * (D * D + 4) * sizeof(float);
