@@ -365,13 +365,19 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
     constexpr int GROUP_TOKENS = K::GROUP * C;
     const float A = a.A[h], bias = a.bias ? a.bias[h] : 0.0f;
     auto turn_of = [&](int group) { return wave / K::WAVES == group % (4 / K::WAVES); };
-    const int mine = 64 * (wave % K::WAVES) + lane;       // this lane's token of a group
+    auto own_token = [&] {                                // this lane's token of a group
+        int again = lane;                                 // (not to be held in registers meanwhile)
+        asm volatile("" : "+v"(again));
+        return 64 * (wave % K::WAVES) + again;
+    };
     auto copy_steps = [&](int64_t t0) {
+        const int mine = own_token();
         if (t0 + mine < end)
             dma_element<Tok<BF>::BYTES>(a.dt + (t0 + mine) * a.dt_stride + h * Tok<BF>::BYTES,
                                         lds_addr(steps + 64 * (wave % K::WAVES)));
     };
     auto put_rates = [&](int group, int64_t t0) {
+        const int mine = own_token();
         const bool there = t0 + mine < end;
         const float x = __uint_as_float(BF ? steps[mine] << 16 : steps[mine]);
         const float delta = there ? scan_delta(x + bias, a.softplus) : 0.0f;
@@ -652,11 +658,13 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
     }
 
     if (MODE == PARTS || (MODE == WHOLE && slot >= 0)) {
+        int again = lane;                       // (the first load's addresses would stay in registers all along)
+        asm volatile("" : "+v"(again));
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            float *row = Sp + K::value_channel(wave, u, l16) * D;
+            float *row = Sp + K::value_channel(wave, u, again & 15) * D;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) *(f32x4 *)(row + K::key_channel(i, g)) = S[i][u];
+            for (int i = 0; i < 8; ++i) *(f32x4 *)(row + K::key_channel(i, again >> 4)) = S[i][u];
         }
     }
     if (MODE == PARTS && tid == 0) p.decays[(int64_t)seg * a.heads_v + h] = exp2_hw((float)total);
