@@ -275,15 +275,6 @@ __device__ __forceinline__ uint32_t lds_addr(const void *p) {
 __device__ __forceinline__ void dma16(const void *g, uint32_t lds_base) {
     asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(g), "s"(lds_base) : "memory");
 }
-// The same for one element of 2 or 4 bytes per lane: lane L writes lds_base + 4 L.
-template <int BYTES>
-__device__ __forceinline__ void dma_element(const void *g, uint32_t lds_base) {
-    if (BYTES == 2) asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_ushort %0, off" :: "v"(g), "s"(lds_base) : "memory");
-    else asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" :: "v"(g), "s"(lds_base) : "memory");
-}
-// Waits until at most N of this wave's memory operations, the youngest, are under way.
-template <int N>
-__device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void wait_vm_all() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 }  // namespace lq

@@ -48,6 +48,13 @@ __device__ __forceinline__ void store_tok(void *p, const float *f) {
     }
 }
 
+// As dma16 (lq_device.hpp), one element of 2 or 4 bytes per lane: lane L writes lds_base + 4 L.
+template <int BYTES>
+__device__ __forceinline__ void dma_element(const void *g, uint32_t lds_base) {
+    if (BYTES == 2) asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_ushort %0, off" :: "v"(g), "s"(lds_base) : "memory");
+    else asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" :: "v"(g), "s"(lds_base) : "memory");
+}
+
 template <bool BF>
 __device__ __forceinline__ float load_tok(const void *p, int64_t i) {
     return BF ? bf2f(((const uint16_t *)p)[i]) : ((const float *)p)[i];

@@ -570,3 +570,45 @@ def test_scan_step_of_many_tiles(dtype):
                           D=y["D"], dt_bias=y["dt_bias"])
     close(o, want, (128 + 24) * U * osize)
     close(st, new, 24 * U * size)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_scan_split_with_slots_and_values_that_are_not_finite(dtype):
+    """The split form: a sequence without a slot, one with a bad slot, and a token that is not finite."""
+    cu, n = packed([700, 3, 1100, 0])
+    x = scan_inputs(n, 2, 1, dtype)
+    x["dt_bias"] -= 1.0
+    d = B.make_dims(4, 2, 1, rule=B.LQ_RULE_ADD)
+    state = rnd(3, 3, 2, 128, 128, scale=0.3)
+    slots = torch.tensor([-1, 7, 1, 2], dtype=torch.int32)
+    old = torch.stack([torch.zeros_like(state[0]), torch.full_like(state[0], float("nan")), state[1], state[2]])
+    want, osize, new, size = R.scan(x["q"], x["k"], x["v"], x["dt"], x["A"], R.lengths(cu, n), x["D"], x["dt_bias"], True, old)
+    st, err = state.cuda(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    clean = run_prompt(d, x, cu, n, dtype, st, True, slots.cuda(), 0, err)
+    close(clean, want, tolerance(osize.nan_to_num(0.0), 1100, dtype))
+    close(st[1], new[2], tolerance(size[2], 1100, dtype))
+    assert torch.equal(st[0].cpu(), state[0]) and torch.equal(st[2].cpu(), state[2])
+    assert B.leapquant_check_error_word(err) == B.LQ_DEVERR_BAD_SLOT
+    for name in ("v", "k", "dt"):
+        y = {a: z.clone() for a, z in x.items()}
+        y[name][500, 0] = float("nan")
+        st2 = state.cuda()
+        o = run_prompt(d, y, cu, n, dtype, st2, True, slots.cuda())
+        assert torch.equal(o[:500], clean[:500]), name
+        assert torch.equal(o[703:], clean[703:]) and torch.equal(st2, st), name     # (the faulty sequence keeps no state)
+        assert o[500:700, 0].isnan().any()
+
+
+def test_scan_split_of_many_sequences():
+    """One long sequence among hundreds of short ones: the segments' numbers are sums over more sequences than threads."""
+    lens = [i % 4 for i in range(270)] + [900] + [1] * 30
+    cu, n = packed(lens)
+    x = scan_inputs(n, 1, 1, BF)
+    state = rnd(9, len(lens), 1, 128, 128, scale=0.3)
+    want, osize, new, size = R.scan(x["q"], x["k"], x["v"], x["dt"], x["A"], R.lengths(cu, n), x["D"], x["dt_bias"], True, state)
+    d = B.make_dims(len(lens), 1, 1, rule=B.LQ_RULE_ADD)
+    assert B.leapquant_scan_workspace_bytes(d, n, BF, 900) > 0
+    st = state.cuda()
+    o = run_prompt(d, x, cu, n, BF, st, True, None, 900)
+    close(o, want, tolerance(osize, 900, BF))
+    close(st, new, tolerance(size, 900, BF))
