@@ -4,6 +4,8 @@
 // Bound: HBM; K multiply-adds per value read.  A thread owns 16 bytes of
 // channels of a run of tokens, whose input rows it reads once into registers;
 // neighbouring lanes own neighbouring channels, so every access is whole lines.
+// 8192 tokens x 8192 channels, bf16, K = 4: 62 us (a large copy's rate: 56); a wave that
+// walks one run only 66.6.  256 tokens x 12288 channels 12.1 us (11.9).
 #include <algorithm>
 
 #include "lq_layer.hpp"

@@ -32,7 +32,8 @@ __device__ __forceinline__ void load8(const char *p, float *f) {
 //
 // Bound: HBM, the state read and written once.  M rows of S^T per thread, 8 key
 // channels each: 16 lanes hold a row, so the output's sum is a DPP row sum, and a
-// workgroup holds 16 M rows, 8 / M workgroups a tile.
+// workgroup holds 16 M rows, 8 / M workgroups a tile.  256 requests x 32 heads, fp32
+// state: 188 us (5.8 TB/s) with one row a thread, 220 with eight.
 template <bool BF, bool SBF, int M>
 __global__ __launch_bounds__(NT) void scan_step_kernel(ScanArgs a) {
     constexpr int PARTS = 8 / M, SB = SBF ? 2 : 4;
@@ -114,6 +115,11 @@ __global__ __launch_bounds__(NT) void scan_step_kernel(ScanArgs a) {
 // state, P, w v) is split into bf16 terms: two for the output (2^-16, it is
 // rounded to bf16 anyway), three for the state (2^-24), which stays fp32.
 // fp32 tokens go through the fp32 matrix instructions.
+//
+// Bound: bf16, the issue of matrix and vector instructions, which do not overlap, beside
+// HBM; fp32, the matrix cores (64% busy in the output pass).  64 ragged prompts, 16383
+// tokens x 32 heads: 182 us, 151 without the products; one of 32768 x 16 heads 235;
+// 2048 fp32 tokens x 32 heads 97.
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -152,7 +158,9 @@ template <bool BF> struct Chunk {
     // Place of a piece in its row: one piece of 16 rows lies in 16 different places
     // of a 256-byte line of banks, and so do the 4 pieces of 4 rows that a
     // transposing read (rows 4 r ..) or a column read of fp32 (rows r, r + 4, ..)
-    // takes at once.
+    // takes at once.  The counters show no conflicts for fp32, but 0.41 of the LDS's
+    // active cycles for bf16, whose reads are not served in runs of 16 lanes; placements
+    // with 64% fewer took the same time (64 ragged prompts x 32 heads 182-186 us).
     __device__ static __forceinline__ int place(int row, int piece) {
         return piece ^ (BF ? 4 * (row & 3) + ((row >> 2) & 3) : row & 15);
     }
