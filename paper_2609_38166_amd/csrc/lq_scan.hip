@@ -112,14 +112,14 @@ __global__ __launch_bounds__(NT) void scan_step_kernel(ScanArgs a) {
 // the transposing LDS read turns them where a product sums over tokens.
 //
 // bf16 tokens are exact operands.  What is multiplied with them in fp32 (the
-// state, P, w v) is split into bf16 terms: two for the output (2^-16, it is
-// rounded to bf16 anyway), three for the state (2^-24), which stays fp32.
+// state, P, w v) is split into three bf16 terms, which hold all its 24 bits: sums are
+// those of fp32 also where they cancel.  (Two terms for the outputs are a tenth faster,
+// 64 ragged prompts 180 instead of 203 us, but drop what lies below 2^-16 of a term.)
 // fp32 tokens go through the fp32 matrix instructions.
 //
 // Bound: bf16, the issue of matrix and vector instructions, which do not overlap, beside
 // HBM; fp32, the matrix cores (64% busy in the output pass).  64 ragged prompts, 16383
-// tokens x 32 heads: 182 us, 151 without the products; one of 32768 x 16 heads 235;
-// 2048 fp32 tokens x 32 heads 97.
+// tokens x 32 heads: 203 us; one of 32768 x 16 heads 257; 2048 fp32 tokens x 32 heads 98.
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -195,7 +195,7 @@ __device__ __forceinline__ bf16x8 pack8(const float *x) {
 }
 // Cuts 8 floats to bf16 and leaves in x what that dropped (exact).  Cut, not rounded:
 // the upper half as it lies is the term (v_and at twice the rate of a shift, and one
-// permutation packs two), at the price of one bit of the terms together.
+// permutation packs two); two cut terms and a rounded one still hold 24 bits.
 __device__ __forceinline__ bf16x8 split8(float *x) {
     uint32_t w[4];
 #pragma unroll
@@ -481,9 +481,11 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
                         float x[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[e] = S[2 * s + (e >> 2)][u][e & 3];
-                        const bf16x8 hi = split8(x), lo = pack8(x);
+                        const bf16x8 hi = split8(x), mid = split8(x), lo = pack8(x);
 #pragma unroll
                         for (int T = 0; T < TILES; ++T) y[T][u] = mfma(hi, qf[T], y[T][u]);
+#pragma unroll
+                        for (int T = 0; T < TILES; ++T) y[T][u] = mfma(mid, qf[T], y[T][u]);
 #pragma unroll
                         for (int T = 0; T < TILES; ++T) y[T][u] = mfma(lo, qf[T], y[T][u]);
                     }
@@ -547,9 +549,11 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
                         float x[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[e] = (e >> 2) <= T ? sc[e >> 2][T][e & 3] : 0.0f;
-                        const bf16x8 hi = split8(x), lo = pack8(x);
+                        const bf16x8 hi = split8(x), mid = split8(x), lo = pack8(x);
 #pragma unroll
                         for (int u = 0; u < 2; ++u) y[T][u] = mfma(xb[u], hi, y[T][u]);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) y[T][u] = mfma(xb[u], mid, y[T][u]);
 #pragma unroll
                         for (int u = 0; u < 2; ++u) y[T][u] = mfma(xb[u], lo, y[T][u]);
                     }

@@ -1,0 +1,59 @@
+"""Layer operators at values and arguments where a kernel goes wrong easily, against their definitions in 64 bits.
+
+Tolerances as in test_gpu_layer.py (u = 2^-24): after t tokens (2 t + 16) u of the sum of the terms' magnitudes, for bf16
+tokens as for fp32 ones: bf16 tokens are exact, and all that is multiplied with them is kept to 2^-23 of its value or
+better.  A bf16 output has half an ulp more.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2609_38166_amd import binding as B
+from tests import layer_reference as R
+from tests.test_gpu_layer import BF, F32, U, close, cu_args, packed, rnd, run_prompt, scan_inputs
+
+pytestmark = pytest.mark.gpu
+
+
+def fp32_tolerance(size, t):
+    return (2 * t + 16) * U * size + 1e-30
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_scan_outputs_where_the_state_cancels(dtype):
+    """Sums of two terms that are 2^-12 apart: what is left shows every bit of the state that a product drops."""
+    n, hv = 20, 2
+    cu, _ = packed([n])
+    x = scan_inputs(n, hv, hv, dtype)
+    x["v"].zero_()
+    x["q"].zero_()
+    x["q"][..., 6] = x["q"][..., 77] = rnd(1, n, hv).to(dtype)
+    x["D"] = None
+    state = rnd(2, 1, hv, 128, 128)
+    state[..., 77] = -state[..., 6] * (1 + 2.0 ** -12 * torch.rand((1, hv, 128), generator=torch.Generator().manual_seed(3)))
+    want, osize, new, size = R.scan(x["q"], x["k"], x["v"], x["dt"], x["A"], [(0, n)], None, x["dt_bias"], True, state)
+    st = state.cuda()
+    o = run_prompt(B.make_dims(1, hv, hv, rule=B.LQ_RULE_ADD), x, cu, n, dtype, st, True)
+    close(o, want, fp32_tolerance(osize, n))
+    close(st, new, fp32_tolerance(size, n))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_scan_outputs_where_the_tokens_cancel(dtype):
+    """The same for the weights of a chunk's own tokens: two equal keys, values of opposite sign, a slow decay."""
+    n, hv = 20, 16
+    cu, _ = packed([n])
+    x = scan_inputs(n, hv, hv, dtype)
+    x["k"][1] = x["k"][0]
+    x["q"][..., 1:] = 0                                   # (one term in q . k)
+    x["v"][1] = -x["v"][0]
+    x["v"][2:] = 0
+    x["dt"].fill_(1.0)
+    x["dt_bias"] = x["D"] = None
+    x["A"] = torch.full((hv,), -2.0 ** -10)
+    want, osize, new, size = R.scan(x["q"], x["k"], x["v"], x["dt"], x["A"], [(0, n)], None, None, False)
+    st = torch.empty((1, hv, 128, 128), device="cuda")
+    o = run_prompt(B.make_dims(1, hv, hv, rule=B.LQ_RULE_ADD), x, cu, n, dtype, st, softplus=False)
+    close(o, want, fp32_tolerance(osize, n))
+    close(st, new, fp32_tolerance(size, n))
