@@ -398,6 +398,8 @@ int32_t leapquant_qk_norm(const lq_qk *n, void *stream);
  * itself) and alpha = exp(delta A), per value head (App. A, the b_t = 0 rows
  * with a scalar gate; beta = delta in leapquant_decode_step's terms)
  *   S_t = alpha_t S_{t-1} + delta_t k_t v_t^T,   o_t = S_t^T q_t + skip v_t.
+ * A dt or dt_bias of -inf masks a token or a head where softplus is taken:
+ * delta = 0, alpha = 1.
  * The shapes are dims': batch sequences, heads_v, heads_k, d_k = d_v = 128, the
  * scalar gate and LQ_RULE_ADD (LQ_EUNSUPPORTED otherwise).
  */

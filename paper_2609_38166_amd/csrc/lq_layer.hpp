@@ -109,7 +109,7 @@ __device__ __forceinline__ float scan_delta(float x, int softplus) {
     p = fmaf(p, z, 1.0f / 5.0f);
     p = fmaf(p, z, 1.0f / 3.0f);
     const float l = 2.0f * fmaf(s * z, p, s);
-    return (x > 0.0f ? x : x - x) + l;              // (x - x: 0, or the NaN that x is)
+    return (x > 0.0f || x != x ? x : 0.0f) + l;     // (0 for x = -inf, a masked token: no step, no decay)
 }
 
 // alpha = exp(x).  Near 1, where a state's memory is long and the roundings of

@@ -57,3 +57,43 @@ def test_scan_outputs_where_the_tokens_cancel(dtype):
     o = run_prompt(B.make_dims(1, hv, hv, rule=B.LQ_RULE_ADD), x, cu, n, dtype, st, softplus=False)
     close(o, want, fp32_tolerance(osize, n))
     close(st, new, fp32_tolerance(size, n))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lens", [[70, 1, 40], [700, 20]], ids=str)
+def test_a_step_of_minus_infinity_masks(lens, dtype):
+    """softplus(-inf) = 0: the token changes nothing and the state keeps; a bias of -inf does that for a whole head."""
+    cu, n = packed(lens)
+    hv, seqs = 3, len(lens)
+    x = scan_inputs(n, hv, 1, dtype)
+    x["dt"][::3, 0] = -math.inf
+    x["dt"][lens[0] - 1] = -math.inf
+    x["dt_bias"][1] = -math.inf
+    state = rnd(9, seqs, hv, 128, 128, scale=0.3)
+    want, osize, new, size = R.scan(x["q"], x["k"], x["v"], x["dt"], x["A"], R.lengths(cu, n), x["D"], x["dt_bias"], True, state)
+    assert want.isfinite().all() and new.isfinite().all()
+    d = B.make_dims(seqs, hv, 1, rule=B.LQ_RULE_ADD)
+    assert (B.leapquant_scan_workspace_bytes(d, n, dtype, max(lens)) > 0) == (max(lens) == 700)       # both forms of the prompt
+    st = state.cuda()
+    o = run_prompt(d, x, cu, n, dtype, st, True, None, max(lens))
+    close(o, want, fp32_tolerance(osize, max(lens)))
+    close(st, new, fp32_tolerance(size, max(lens)))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_step_of_minus_infinity_masks_single_tokens(dtype):
+    batch, hv = 3, 4
+    x = scan_inputs(batch, hv, 1, dtype)
+    x["dt"][0, 1] = x["dt_bias"][2] = -math.inf
+    state = rnd(9, batch, hv, 128, 128)
+    want, osize, new, size = R.scan(x["q"], x["k"], x["v"], x["dt"], x["A"], [(b, b + 1) for b in range(batch)], x["D"],
+                                    x["dt_bias"], True, state)
+    d, y, st = B.make_dims(batch, hv, 1, rule=B.LQ_RULE_ADD), cu_args(x), state.cuda()
+    o = torch.empty((batch, hv, 128), dtype=dtype, device="cuda")
+    B.leapquant_scan_step(d, st, y["q"], y["k"], y["v"], y["dt"], y["A"], o, D=y["D"], dt_bias=y["dt_bias"])
+    close(o, want, (128 + 24) * U * osize)
+    close(st, new, 24 * U * size)
+    alpha, beta = (torch.empty((batch, hv), device="cuda") for _ in range(2))
+    B.leapquant_scan_gates(d, y["dt"], y["A"], alpha, beta, dt_bias=y["dt_bias"])
+    for b, h in ((0, 1), (0, 2), (1, 2), (2, 2)):
+        assert float(alpha[b, h]) == 1.0 and float(beta[b, h]) == 0.0
