@@ -299,8 +299,101 @@ __device__ __forceinline__ void find_segment(const ScanArgs &a, int seg, int len
     }
 }
 
+__device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
+
+// Whether what a wave's results that are not finite come from has NaN, but no infinity: its
+// tokens' keys, values and queries, their steps, the state they started from.
 template <bool BF, int MODE>
-__global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
+__device__ __forceinline__ bool only_nan(const ScanArgs &a, int64_t begin, int64_t end, int h, int wave, int lane,
+                                         const float *state, bool given) {
+    bool nan = false, inf = false;
+    auto see = [&](float x) {
+        nan |= x != x;
+        inf |= fabsf(x) == INFINITY;
+    };
+    constexpr int V = Tok<BF>::V, PIECES = D / V;
+    const int64_t piece = lane % PIECES * 16, key = (int64_t)(h / a.group) * D * Tok<BF>::BYTES + piece;
+    const int64_t value = (int64_t)h * D * Tok<BF>::BYTES + piece;
+#pragma unroll 4
+    for (int64_t t = begin + lane / PIECES; t < end; t += 64 / PIECES) {
+        float x[3][V];
+        unpack16<BF>(*(const uint4 *)(a.k + t * a.k_stride + key), x[0]);
+        unpack16<BF>(*(const uint4 *)(a.v + t * a.v_stride + value), x[1]);
+        if (MODE != PARTS) unpack16<BF>(*(const uint4 *)(a.q + t * a.q_stride + key), x[2]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            see(x[0][i]);
+            see(x[1][i]);
+            if (MODE != PARTS) see(x[2][i]);
+        }
+    }
+    const float bias = a.bias ? a.bias[h] : 0.0f;
+    for (int64_t t = begin + lane; t < end; t += 64) see(scan_delta(load_tok<BF>(a.dt + t * a.dt_stride, h) + bias, a.softplus));
+    see(a.A[h]);
+    if (given)
+        for (int i = lane; i < 32 * D; i += 64) see(state[32 * wave * D + i]);
+    return __any(nan) && !__any(inf);
+}
+
+// The 32 value channels of wave `wave` of head h over tokens [begin, end) by the
+// recurrence itself, token by token as scan_step does, from the state s (8 rows of S^T per
+// lane: 32 wave + (lane >> 4) + 4 m, 8 key channels each).  Outputs and entries of the final
+// state (NULL: not kept) are replaced where the stored ones are not finite.  For segments
+// whose products met an infinity: a cut into terms leaves inf - inf there, a weight rounded
+// to zero 0 inf, and neither is in the recurrence.  16 x 1024 tokens x 32 heads, the values
+// of one token infinite: 1.7 ms instead of 0.17.  (Looked for in the
+// operands, infinities would cost every chunk; the sum over results that finds them is within 1%.)
+template <bool BF, int MODE>
+__device__ __forceinline__ void walk_by_token(const ScanArgs &a, int64_t begin, int64_t end, int h, int wave, int lane,
+                                              float (*s)[8], float *state) {
+    const int l16 = lane & 15, r0 = 32 * wave + (lane >> 4);
+    const float A = a.A[h], bias = a.bias ? a.bias[h] : 0.0f, skip = a.skip ? a.skip[h] : 0.0f;
+    const int64_t kc = ((int64_t)(h / a.group) * D + 8 * l16) * Tok<BF>::BYTES;
+#pragma unroll 1
+    for (int64_t t = begin; t < end; ++t) {
+        float k[8], q[8], v[8], was[8];
+        char *o = a.o + t * a.o_stride;
+        load8<BF>(a.k + t * a.k_stride + kc, k);
+        if (MODE != PARTS) load8<BF>(a.q + t * a.q_stride + kc, q);
+#pragma unroll
+        for (int m = 0; m < 8; ++m) {
+            v[m] = load_tok<BF>(a.v + t * a.v_stride, (int64_t)h * D + r0 + 4 * m);
+            if (MODE != PARTS) was[m] = load_tok<BF>(o, (int64_t)h * D + r0 + 4 * m);
+        }
+        const float delta = scan_delta(load_tok<BF>(a.dt + t * a.dt_stride, h) + bias, a.softplus);
+        const float alpha = scan_alpha(delta * A);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) k[j] *= delta;
+#pragma unroll
+        for (int m = 0; m < 8; ++m) {
+            const int64_t at = (int64_t)h * D + r0 + 4 * m;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[m][j] = fmaf(k[j], v[m], alpha * s[m][j]);
+            if (MODE != PARTS) {
+                float y = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y = fmaf(s[m][j], q[j], y);
+                y = row16_sum(y);
+                if (a.skip) y = fmaf(skip, v[m], y);
+                if (l16 == 0 && !is_finite(was[m])) {
+                    if (BF) ((uint16_t *)o)[at] = (uint16_t)pk_bf16(y, y);
+                    else ((float *)o)[at] = y;
+                }
+            }
+        }
+    }
+    if (MODE == OUTPUT || !state) return;
+#pragma unroll
+    for (int m = 0; m < 8; ++m) {
+        float *row = state + (r0 + 4 * m) * D + 8 * l16;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (!is_finite(row[j])) row[j] = s[m][j];
+    }
+}
+
+template <bool BF, int MODE>
+__global__ __launch_bounds__(256, !BF && MODE == PARTS ? 4 : 3) void scan_prompt_kernel(PromptArgs p) {
     using K = Chunk<BF>;
     constexpr int C = K::C, TILES = K::TILES;
     constexpr int ARRAYS = MODE == PARTS ? 2 : 3;           // keys, values, queries
@@ -410,8 +503,8 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
     const int slot = MODE == WHOLE ? state_row(a.state, a.slots, b, a.n_slots, a.err) : NO_SLOT;
     float *Sp = MODE == WHOLE ? (float *)a.state + ((int64_t)slot * a.heads_v + h) * D * D
                               : p.parts + ((int64_t)seg * a.heads_v + h) * D * D;
+    const bool given = MODE == OUTPUT || (MODE == WHOLE && slot >= 0 && a.carry);
     {
-        const bool given = MODE == OUTPUT || (MODE == WHOLE && slot >= 0 && a.carry);
         const float fill = MODE == WHOLE && slot == BAD_SLOT ? nanf32() : 0.0f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -431,6 +524,7 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
         put_rates(0, begin);
     }
     double total = 0.0;                                   // log2 decay of the segment
+    float odd_sum = 0.0f;                                 // NaN once a result is not finite
     int chunk = 0;
     for (int64_t t0 = begin; t0 < end; t0 += C, ++chunk) {
         // this chunk's rows have arrived, and nobody reads the last one's any more
@@ -606,6 +700,8 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) out[e] = fmaf(skip, x[e], out[e]);
                 }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) odd_sum = fmaf(out[e], 0.0f, odd_sum);
                 if (t0 + t < end) {
                     char *row = a.o + (t0 + t) * a.o_stride + (int64_t)h * K::ROW;
                     if constexpr (BF) {
@@ -669,15 +765,47 @@ __global__ __launch_bounds__(256, 3) void scan_prompt_kernel(PromptArgs p) {
         }
     }
 
-    if (MODE == PARTS || (MODE == WHOLE && slot >= 0)) {
-        int again = lane;                       // (the first load's addresses would stay in registers all along)
-        asm volatile("" : "+v"(again));
+    if (MODE != OUTPUT) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) odd_sum = fmaf(S[i][u][r], 0.0f, odd_sum);
+    }
+    int again = lane;                           // (the first load's addresses would stay in registers all along)
+    asm volatile("" : "+v"(again));
+    const bool keeps = MODE == PARTS || (MODE == WHOLE && slot >= 0);
+    // (a sequence that starts from NaN for want of a slot is NaN throughout, and NaN alone the
+    // products carry on as the recurrence does)
+    // What an infinity met is made again by the recurrence, whose arguments are read again
+    // (none of them is held for this throughout the kernel).  A sequence that starts from NaN
+    // for want of a slot is NaN throughout, and NaN alone the products carry on as it does.
+    const PromptArgs *args = (const PromptArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(args));
+    const bool walks = __any(odd_sum != odd_sum) && (MODE != WHOLE || slot != BAD_SLOT) &&
+                       !only_nan<BF, MODE>(args->s, begin, end, h, wave, again, Sp, given);
+    float start[8][8];
+    if (walks) {
+#pragma unroll
+        for (int m = 0; m < 8; ++m) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) start[m][j] = 0.0f;
+            if (given) load8<false>((const char *)(Sp + (32 * wave + (again >> 4) + 4 * m) * D + 8 * (again & 15)), start[m]);
+        }
+        wait_vm_all();
+    }
+    if (keeps) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float *row = Sp + K::value_channel(wave, u, again & 15) * D;
 #pragma unroll
             for (int i = 0; i < 8; ++i) *(f32x4 *)(row + K::key_channel(i, again >> 4)) = S[i][u];
         }
+    }
+    if (walks) {
+        wait_vm_all();                          // outputs and state are stored
+        walk_by_token<BF, MODE>(args->s, begin, end, h, wave, again, start, keeps ? Sp : nullptr);
     }
     if (MODE == PARTS && tid == 0) p.decays[(int64_t)seg * a.heads_v + h] = exp2_hw((float)total);
 }
@@ -713,7 +841,10 @@ __global__ __launch_bounds__(256) void scan_join_kernel(PromptArgs p) {
     for (int s = first; s < last; ++s, part += step, decay += a.heads_v) {
         const f32x4 own = *(const f32x4 *)part;
         *(f32x4 *)part = S;
-        S = S * *decay + own;
+        // (a decay is above zero however small: an infinity stays one where it is rounded to 0)
+        const float by = *decay;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[i] = (by == 0.0f && !is_finite(S[i]) ? S[i] : S[i] * by) + own[i];
     }
     if (slot >= 0) *(f32x4 *)St = S;
 }

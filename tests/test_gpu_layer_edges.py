@@ -97,3 +97,52 @@ def test_a_step_of_minus_infinity_masks_single_tokens(dtype):
     B.leapquant_scan_gates(d, y["dt"], y["A"], alpha, beta, dt_bias=y["dt_bias"])
     for b, h in ((0, 1), (0, 2), (1, 2), (2, 2)):
         assert float(alpha[b, h]) == 1.0 and float(beta[b, h]) == 0.0
+
+
+def same_values(got, want, tol):
+    """NaN and infinities in the same places, the finite ones within tol and the rounding of a bf16 result."""
+    g = got.double().cpu()
+    if got.dtype == BF:
+        tol = tol + want.abs().nan_to_num(0.0, 0.0, 0.0) * 2.0 ** -8
+    assert torch.equal(g.isnan(), want.isnan()), (int(g.isnan().sum()), int(want.isnan().sum()))
+    assert torch.equal(g[want.isinf()], want[want.isinf()])
+    fin = want.isfinite()
+    assert g[fin].isfinite().all() and ((g - want).abs()[fin] <= (tol + 0 * want)[fin]).all()
+
+
+@pytest.mark.parametrize("kind", ["state", "value", "value, strong decay", "key", "query", "step"])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lens", [[70, 40], [700, 20]], ids=str)
+def test_scan_with_infinities_is_the_recurrence(lens, dtype, kind):
+    """An infinity stays one in the state, token by token, also where a decay over many tokens rounds to zero."""
+    cu, n = packed(lens)
+    x = scan_inputs(n, 2, 1, dtype)
+    state = rnd(9, 2, 2, 128, 128, scale=0.3)
+    x["dt"] *= 0.1
+    if "strong" in kind:
+        x["A"] = torch.tensor([-200.0, -150.0])           # about e^-9 a token: 16 of them are below fp32's range
+    clean_state = state.clone().cuda()
+    d = B.make_dims(2, 2, 1, rule=B.LQ_RULE_ADD)
+    assert (B.leapquant_scan_workspace_bytes(d, n, dtype, max(lens)) > 0) == (max(lens) == 700)
+    clean = run_prompt(d, x, cu, n, dtype, clean_state, True, None, max(lens))
+    if kind == "state":
+        state[0, 0, 5, 9], state[0, 1, 7, 3], state[1, 0, 100, 127] = math.inf, -math.inf, math.inf
+    elif "value" in kind:
+        x["v"][10, 0, 5] = math.inf
+        x["v"][lens[0] + 17, 1, 90] = -math.inf
+    elif kind == "key":
+        x["k"][10, 0, 9] = math.inf
+    elif kind == "query":
+        x["q"][10, 0, 9] = -math.inf
+    else:
+        x["dt"][10, 1] = math.inf
+    want, osize, new, size = R.scan(x["q"], x["k"], x["v"], x["dt"], x["A"], R.lengths(cu, n), x["D"], x["dt_bias"], True, state)
+    st = state.cuda()
+    o = run_prompt(d, x, cu, n, dtype, st, True, None, max(lens))
+    same_values(o, want, fp32_tolerance(osize.nan_to_num(0.0, 0.0, 0.0), max(lens)))
+    same_values(st, new, fp32_tolerance(size.nan_to_num(0.0, 0.0, 0.0), max(lens)))
+    # what the infinity does not reach keeps its bits
+    fin = want.isfinite().cuda()
+    assert torch.equal(o[fin], clean[fin])
+    fin = new.isfinite().cuda()
+    assert torch.equal(st[fin], clean_state[fin])
