@@ -397,7 +397,8 @@ __global__ __launch_bounds__(256, !BF && MODE == PARTS ? 4 : 3) void scan_prompt
     using K = Chunk<BF>;
     constexpr int C = K::C, TILES = K::TILES;
     constexpr int ARRAYS = MODE == PARTS ? 2 : 3;           // keys, values, queries
-    __shared__ __attribute__((aligned(16))) char rows[2][ARRAYS][K::BYTES];
+    // (operands are addressed by exclusive ors within a row: it starts at a multiple of its size)
+    __shared__ __attribute__((aligned(K::ROW))) char rows[2][ARRAYS][K::BYTES];
     __shared__ uint32_t steps[K::GROUP * C];                // dt of a group as it lies in memory
     __shared__ typename K::Rates rates[2][K::GROUP];
     const ScanArgs &a = p.s;
