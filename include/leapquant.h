@@ -430,8 +430,10 @@ typedef struct {
     size_t workspace_bytes;
 } lq_scan;
 
-/* leapquant_scan_workspace_bytes -- host only: workspace that
- * leapquant_scan_prompt needs for these shapes, tokens and max_len (may be 0). */
+/* leapquant_scan_workspace_bytes -- host only: workspace (may be 0) that
+ * leapquant_scan_prompt needs: with max_len > 0 for a call of these dims, tokens and
+ * max_len; with max_len = 0 for every call of these dims and type with at most so many
+ * tokens, whatever its max_len, so that one workspace serves prompts of all lengths. */
 int32_t leapquant_scan_workspace_bytes(const lq_dims *dims, const lq_scan *s, size_t *bytes_out);
 
 /* leapquant_scan_prompt -- all tokens of packed sequences, fp32 states.  Tokens and

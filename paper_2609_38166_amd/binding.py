@@ -603,7 +603,7 @@ def leapquant_scan_prompt(dims: lq_dims, q, k, v, dt, A, o, cu_seqlens, D=None, 
             return _check(status, "leapquant_scan_prompt")
     if _seqs(cu_seqlens) != dims.batch:
         raise ValueError(f"cu_seqlens holds {_seqs(cu_seqlens)} sequences, dims.batch is {dims.batch}")
-    a = _scan_args(dims, q, k, v, dt, A, o, state, cu_seqlens, D, dt_bias, softplus, carry, slots, max_len, err)
+    a = _scan_args(dims, q, k, v, dt, A, o, state, cu_seqlens, D, dt_bias, softplus, carry, slots, max_len or v.shape[0], err)
     need = C.c_size_t(0)
     _check(_lib().leapquant_scan_workspace_bytes(C.byref(dims), C.byref(a), C.byref(need)), "leapquant_scan_workspace_bytes")
     if need.value:
@@ -617,7 +617,8 @@ def leapquant_scan_prompt(dims: lq_dims, q, k, v, dt, A, o, cu_seqlens, D=None, 
 
 
 def leapquant_scan_workspace_bytes(dims: lq_dims, tokens, dtype=torch.bfloat16, max_len=0) -> int:
-    """Workspace that leapquant_scan_prompt needs for these shapes."""
+    """Workspace that leapquant_scan_prompt needs: for a call of these tokens and max_len, or, with
+    max_len = 0, for every call with at most so many tokens."""
     need = C.c_size_t(0)
     a = lq_scan(tokens=tokens, dtype=_TOKEN[dtype], max_len=max_len)
     _check(_lib().leapquant_scan_workspace_bytes(C.byref(dims), C.byref(a), C.byref(need)), "leapquant_scan_workspace_bytes")

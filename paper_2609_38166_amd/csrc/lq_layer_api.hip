@@ -165,8 +165,10 @@ int32_t leapquant_scan_workspace_bytes(const lq_dims *d, const lq_scan *s, size_
 int32_t leapquant_scan_prompt(const lq_dims *d, const lq_scan *s, void *stream) {
     int32_t e = check_scan(d, s, 0);
     if (e != LQ_OK) return e;
-    const size_t need = lq::scan_workspace_bytes(*d, *s);
-    if (need) {
+    lq_scan one = *s;                           // (this call alone, not all that max_len = 0 stands for)
+    if (one.max_len == 0) one.max_len = (int32_t)one.tokens;
+    if (lq::scan_workspace_bytes(*d, one)) {
+        const size_t need = lq::scan_workspace_bytes(*d, *s);
         if ((e = check(s->workspace, 16)) != LQ_OK) return e;
         if (s->workspace_bytes < need) return LQ_EINVAL;
     }

@@ -906,17 +906,30 @@ struct Split {
     int64_t segments;
     size_t bytes;
 };
+constexpr int64_t FULL = 512;                   // workgroups
+size_t split_bytes(const lq_dims &d, int64_t segments) { return (size_t)segments * d.heads_v * (D * D + 4) * sizeof(float); }
+int64_t least_chain(const lq_scan &s) { return s.dtype == LQ_TOKEN_BF16 ? 4 : 3; }      // segments, of the longest sequence
+
 Split split_of(const lq_dims &d, const lq_scan &s) {
-    constexpr int64_t FULL = 512;               // workgroups
     Split r{0, d.batch, 0};
     const int64_t longest = s.max_len > 0 && s.max_len < s.tokens ? s.max_len : s.tokens;
     if ((int64_t)d.batch * d.heads_v >= FULL) return r;
     const int64_t length = std::max<int64_t>((s.tokens * d.heads_v / FULL + 63) / 64 * 64, 64);
-    if (longest <= (s.dtype == LQ_TOKEN_BF16 ? 4 : 3) * length) return r;
+    if (longest <= least_chain(s) * length) return r;
     r.length = (int32_t)length;
     r.segments = s.tokens / length + d.batch;   // each sequence's last segment may be short
-    r.bytes = (size_t)r.segments * d.heads_v * (D * D + 4) * sizeof(float);
+    r.bytes = split_bytes(d, r.segments);
     return r;
+}
+
+// The most that split_of gives for up to s.tokens tokens and any max_len.  A segment's length
+// is rounded up to 64, so their number falls each time a longer one is taken: it is largest
+// for the most tokens that the shortest length, 64, serves; where those are not cut, no
+// others are.
+size_t most_split_bytes(const lq_dims &d, const lq_scan &s) {
+    if ((int64_t)d.batch * d.heads_v >= FULL) return 0;
+    const int64_t tokens = std::min(s.tokens, (65 * FULL - 1) / d.heads_v);
+    return tokens > least_chain(s) * 64 ? split_bytes(d, tokens / 64 + d.batch) : 0;
 }
 
 template <bool BF>
@@ -962,7 +975,9 @@ hipError_t launch_step(const lq_dims &d, const lq_scan &s, hipStream_t st) {
 
 }  // namespace
 
-size_t scan_workspace_bytes(const lq_dims &d, const lq_scan &s) { return split_of(d, s).bytes; }
+size_t scan_workspace_bytes(const lq_dims &d, const lq_scan &s) {
+    return s.max_len > 0 ? split_of(d, s).bytes : most_split_bytes(d, s);
+}
 
 hipError_t launch_scan_prompt(const lq_dims &d, const lq_scan &s, hipStream_t st) {
     return s.dtype == LQ_TOKEN_BF16 ? launch_prompt<true>(d, s, st) : launch_prompt<false>(d, s, st);

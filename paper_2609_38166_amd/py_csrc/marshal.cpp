@@ -11,6 +11,8 @@
 // words what it refuses.  Nothing is kept from one call for the next.
 #include <Python.h>
 
+#include <algorithm>
+
 #include <c10/hip/HIPStream.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -378,7 +380,7 @@ PyObject *scan(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (!vec(a[15], d.batch, I32, true, &c.slots) || !error_word(a[18], &c.err)) return false;
         const long max_len = PyLong_AsLong(a[16]);
         if (PyErr_Occurred() || max_len < INT32_MIN || max_len > INT32_MAX) return false;
-        c.max_len = (int32_t)max_len;
+        c.max_len = (int32_t)(max_len ? max_len : std::min<int64_t>(T, INT32_MAX));     // (the need of this call alone)
         c.softplus = PyObject_IsTrue(a[11]);
         c.carry = PyObject_IsTrue(a[14]);
         c.tokens = T;

@@ -146,3 +146,31 @@ def test_scan_with_infinities_is_the_recurrence(lens, dtype, kind):
     assert torch.equal(o[fin], clean[fin])
     fin = new.isfinite().cuda()
     assert torch.equal(st[fin], clean_state[fin])
+
+
+def test_one_workspace_serves_prompts_of_all_lengths():
+    """Sized for the longest prompt; on a stream of the caller's, which has to bring it."""
+    hv = 64
+    d = B.make_dims(1, hv, 1, rule=B.LQ_RULE_ADD)
+    ws = torch.empty(B.leapquant_scan_workspace_bytes(d, 2056), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    for n in (1, 256, 512, 520, 1024, 2048, 2056):
+        y = cu_args(scan_inputs(n, hv, 1, BF))
+        cu = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+        got = []
+        for max_len in (0, n, None):
+            o = torch.empty((n, hv, 128), dtype=BF, device="cuda")
+            torch.cuda.synchronize()
+            kw = {"stream": side, "workspace": ws, "max_len": max_len} if max_len is not None else {}
+            B.leapquant_scan_prompt(d, y["q"], y["k"], y["v"], y["dt"], y["A"], o, cu, D=y["D"], dt_bias=y["dt_bias"], **kw)
+            torch.cuda.synchronize()
+            got.append(o)
+        assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[2])
+    # a call that is not cut needs none, whatever others of its size may
+    d = B.make_dims(1, 100, 1, rule=B.LQ_RULE_ADD)
+    assert B.leapquant_scan_workspace_bytes(d, 400) > 0 and B.leapquant_scan_workspace_bytes(d, 400, max_len=400) == 0
+    y = cu_args(scan_inputs(400, 100, 1, BF))
+    o = torch.empty((400, 100, 128), dtype=BF, device="cuda")
+    torch.cuda.synchronize()
+    B.leapquant_scan_prompt(d, y["q"], y["k"], y["v"], y["dt"], y["A"], o, torch.tensor([0, 400], dtype=torch.int32).cuda(), stream=side)
+    side.synchronize()
