@@ -603,7 +603,8 @@ def leapquant_scan_prompt(dims: lq_dims, q, k, v, dt, A, o, cu_seqlens, D=None, 
             return _check(status, "leapquant_scan_prompt")
     if _seqs(cu_seqlens) != dims.batch:
         raise ValueError(f"cu_seqlens holds {_seqs(cu_seqlens)} sequences, dims.batch is {dims.batch}")
-    a = _scan_args(dims, q, k, v, dt, A, o, state, cu_seqlens, D, dt_bias, softplus, carry, slots, max_len or v.shape[0], err)
+    a = _scan_args(dims, q, k, v, dt, A, o, state, cu_seqlens, D, dt_bias, softplus, carry, slots,
+                   min(v.shape[0], 2**31 - 1) if max_len == 0 else max_len, err)
     need = C.c_size_t(0)
     _check(_lib().leapquant_scan_workspace_bytes(C.byref(dims), C.byref(a), C.byref(need)), "leapquant_scan_workspace_bytes")
     if need.value:
