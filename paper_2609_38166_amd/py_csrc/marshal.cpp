@@ -233,6 +233,18 @@ bool error_word(PyObject *o, int32_t **p) {
     return true;
 }
 
+// False, True, 0 or 1; what else int() makes of a flag, or refuses, is the Python path's.
+bool flag(PyObject *o, int32_t *p) {
+    if (o == Py_True || o == Py_False) {
+        *p = o == Py_True;
+        return true;
+    }
+    if (!PyLong_CheckExact(o)) return false;
+    const long x = PyLong_AsLong(o);
+    *p = (int32_t)x;
+    return x == 0 || x == 1;
+}
+
 constexpr at::ScalarType F = at::ScalarType::Float, I32 = at::ScalarType::Int;
 
 // conv(fn, x, weight, out, cu_seqlens or None (the step), bias, silu, state, carry, slots, err)
@@ -265,8 +277,7 @@ PyObject *conv(PyObject *, PyObject *const *a, Py_ssize_t n) {
         c.seqs = (int32_t)seqs;
         c.channels = (int32_t)size[1];
         c.width = (int32_t)width;
-        c.silu = PyObject_IsTrue(a[6]);
-        c.carry = PyObject_IsTrue(a[8]);
+        if (!flag(a[6], &c.silu) || !flag(a[8], &c.carry)) return false;
         c.tokens = size[0];
         using Fn = int32_t (*)(const lq_conv *, void *);
         const Fn fn = (Fn)PyLong_AsVoidPtr(a[0]);
@@ -322,7 +333,7 @@ PyObject *qk_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
         c.q_scale = (float)PyFloat_AsDouble(a[9]);
         if (PyErr_Occurred() || norm < INT32_MIN || norm > INT32_MAX) return false;
         c.norm = (int32_t)norm;
-        c.interleaved = PyObject_IsTrue(a[13]);
+        if (!flag(a[13], &c.interleaved)) return false;
         c.tokens = qs[0];
         c.heads_q = (int32_t)qs[1];
         c.heads_k = (int32_t)hk;
@@ -381,8 +392,7 @@ PyObject *scan(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const long max_len = PyLong_AsLong(a[16]);
         if (PyErr_Occurred() || max_len < INT32_MIN || max_len > INT32_MAX) return false;
         c.max_len = (int32_t)(max_len ? max_len : std::min<int64_t>(T, INT32_MAX));     // (the need of this call alone)
-        c.softplus = PyObject_IsTrue(a[11]);
-        c.carry = PyObject_IsTrue(a[14]);
+        if (!flag(a[11], &c.softplus) || !flag(a[14], &c.carry)) return false;
         c.tokens = T;
         at::Tensor own;                 // freed into the allocator's pool of this stream after the launch
         if (!step) {

@@ -174,3 +174,36 @@ def test_one_workspace_serves_prompts_of_all_lengths():
     torch.cuda.synchronize()
     B.leapquant_scan_prompt(d, y["q"], y["k"], y["v"], y["dt"], y["A"], o, torch.tensor([0, 400], dtype=torch.int32).cuda(), stream=side)
     side.synchronize()
+
+
+class NoTruth:
+    def __bool__(self):
+        raise RuntimeError("no truth value")
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("flag", [2, -1, NoTruth(), "yes", None], ids=["2", "-1", "raises", "text", "none"])
+def test_flags_are_refused_alike_by_the_native_and_the_python_path(flag, native, monkeypatch):
+    assert B.lib() and B._M is not B._NoMarshal
+    if not native:
+        monkeypatch.setattr(B, "_M", B._NoMarshal)
+    n = 4
+    y = cu_args(scan_inputs(n, 2, 2, BF))
+    d = B.make_dims(1, 2, 2, rule=B.LQ_RULE_ADD)
+    cu = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    o, st = torch.empty((n, 2, 128), dtype=BF, device="cuda"), torch.zeros((1, 2, 128, 128), device="cuda")
+    x, w, cs = rnd(1, n, 64).cuda(), rnd(2, 64, 4).cuda(), torch.zeros((1, 3, 64), device="cuda")
+    cos = torch.ones((n, 32), device="cuda")
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    tokens = (y["q"], y["k"], y["v"], y["dt"], y["A"], o)
+    for call in (lambda f: B.leapquant_conv_prompt(x, w, torch.empty_like(x), cu, silu=f),
+                 lambda f: B.leapquant_conv_prompt(x, w, torch.empty_like(x), cu, state=cs, carry=f),
+                 lambda f: B.leapquant_conv_step(x[:1], w, torch.empty_like(x[:1]), cs, silu=f),
+                 lambda f: B.leapquant_qk_norm(y["q"], None, o, None, cos=cos, sin=cos, positions=pos, interleaved=f),
+                 lambda f: B.leapquant_scan_prompt(d, *tokens, cu, softplus=f),
+                 lambda f: B.leapquant_scan_prompt(d, *tokens, cu, state=st, carry=f),
+                 lambda f: B.leapquant_scan_step(d, st, *(t[:1] for t in tokens[:4]), y["A"], o[:1], softplus=f)):
+        for good in (True, False, 0, 1):
+            call(good)
+        with pytest.raises(B.LeapQuantError if isinstance(flag, int) else (TypeError, ValueError)):
+            call(flag)
