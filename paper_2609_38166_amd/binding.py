@@ -511,7 +511,7 @@ def leapquant_conv_prompt(x, weight, out, cu_seqlens, bias=None, silu=True, stat
     """Short causal convolution of packed sequences: x, out [tokens, channels], weight
     [channels, width], cu_seqlens int32 [sequences + 1]; state [slots, width-1, channels]
     of x's type, read if `carry`, holds the last inputs afterwards."""
-    if stream is None and (_M or _lib()):
+    if stream is None and cu_seqlens is not None and (_M or _lib()):
         status = _M.conv(_FN["leapquant_conv_prompt"], x, weight, out, cu_seqlens, bias, silu, state, carry, slots, err)
         if status is not None:
             return _check(status, "leapquant_conv_prompt")
@@ -596,7 +596,7 @@ def leapquant_scan_prompt(dims: lq_dims, q, k, v, dt, A, o, cu_seqlens, D=None, 
     max_len, the longest sequence, lets the work be split better where it is known.  The
     workspace is allocated here unless a uint8 tensor is given; a stream of the caller's
     needs one."""
-    if stream is None and (_M or _lib()):
+    if stream is None and cu_seqlens is not None and (_M or _lib()):
         status = _M.scan(_FN["leapquant_scan_prompt"], _FN["leapquant_scan_workspace_bytes"], dims, q, k, v, dt, A, o, D, dt_bias,
                          softplus, state, cu_seqlens, carry, slots, max_len, workspace, err)
         if status is not None:

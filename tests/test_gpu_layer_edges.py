@@ -207,3 +207,17 @@ def test_flags_are_refused_alike_by_the_native_and_the_python_path(flag, native,
             call(good)
         with pytest.raises(B.LeapQuantError if isinstance(flag, int) else (TypeError, ValueError)):
             call(flag)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_prompts_without_cu_seqlens_are_refused_alike(native, monkeypatch):
+    assert B.lib() and B._M is not B._NoMarshal
+    if not native:
+        monkeypatch.setattr(B, "_M", B._NoMarshal)
+    y = cu_args(scan_inputs(4, 2, 2, BF))
+    o, st = torch.empty((4, 2, 128), dtype=BF, device="cuda"), torch.zeros((1, 2, 128, 128), device="cuda")
+    x, w, cs = rnd(1, 4, 64).cuda(), rnd(2, 64, 4).cuda(), torch.zeros((4, 3, 64), device="cuda")
+    with pytest.raises(ValueError, match="cu_seqlens is required"):
+        B.leapquant_conv_prompt(x, w, torch.empty_like(x), None, state=cs)
+    with pytest.raises(ValueError, match="cu_seqlens is required"):
+        B.leapquant_scan_prompt(B.make_dims(1, 2, 2, rule=B.LQ_RULE_ADD), y["q"], y["k"], y["v"], y["dt"], y["A"], o, None, state=st)
