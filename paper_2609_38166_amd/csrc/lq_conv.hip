@@ -133,6 +133,7 @@ __global__ __launch_bounds__(256) void conv_prompt_kernel(ConvArgs a) {
     if (blockIdx.x == 0) check_seqlens(a.cu, a.seqs, a.tokens, a.err, threadIdx.x, 256);
     if (block >= a.blocks_t) {
         // empty sequences without carry: their state becomes zero
+        if (a.carry) return;
         const int b = (block - a.blocks_t) * 4 + wave;
         if (b >= a.seqs) return;
         const Span s = sequence_span(a.cu, b, a.tokens);
@@ -286,8 +287,11 @@ hipError_t launch(ConvArgs a, bool step, hipStream_t st) {
         const int64_t runs = std::max<int64_t>((groups + round - 1) / round, 1);
         a.runs = runs > 8 ? 2 : (int)runs;
         a.blocks_t = (int)((a.tokens + 4 * RUN * a.runs - 1) / (4 * RUN * a.runs));
-        const int extra = a.state && !a.carry ? (a.seqs + 3) / 4 : 0;
-        if (a.blocks_t + extra == 0) return hipSuccess;
+        int extra = a.state && !a.carry ? (a.seqs + 3) / 4 : 0;
+        if (a.blocks_t + extra == 0) {
+            if (!a.err) return hipSuccess;
+            extra = 1;                          // no tokens: the lengths are checked all the same
+        }
         hipLaunchKernelGGL((conv_prompt_kernel<K, BF, OBF>), dim3(a.blocks_c * (a.blocks_t + extra)), dim3(256), 0, st, a);
     }
     return hipGetLastError();

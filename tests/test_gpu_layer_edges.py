@@ -221,3 +221,18 @@ def test_prompts_without_cu_seqlens_are_refused_alike(native, monkeypatch):
         B.leapquant_conv_prompt(x, w, torch.empty_like(x), None, state=cs)
     with pytest.raises(ValueError, match="cu_seqlens is required"):
         B.leapquant_scan_prompt(B.make_dims(1, 2, 2, rule=B.LQ_RULE_ADD), y["q"], y["k"], y["v"], y["dt"], y["A"], o, None, state=st)
+
+
+@pytest.mark.parametrize("carry", [False, True])
+def test_conv_of_no_tokens_reports_lengths_that_claim_some(carry):
+    x, w = rnd(1, 5, 64).cuda(), rnd(2, 64, 4).cuda()
+    state = rnd(3, 2, 3, 64)
+    for cu, bits in (([0, 0, 0], 0), ([0, 5, 5], B.LQ_DEVERR_BAD_SEQLENS), ([0, 0, -1], B.LQ_DEVERR_BAD_SEQLENS)):
+        for st in (state.cuda(), None):
+            if st is None and carry:
+                continue
+            err = torch.zeros(1, dtype=torch.int32, device="cuda")
+            B.leapquant_conv_prompt(x[:0], w, x[:0], torch.tensor(cu, dtype=torch.int32).cuda(), state=st, carry=carry, err=err)
+            assert B.leapquant_check_error_word(err) == bits
+            if st is not None:
+                assert torch.equal(st.cpu(), state if carry else torch.zeros_like(state))
