@@ -130,7 +130,12 @@ __global__ __launch_bounds__(256) void conv_prompt_kernel(ConvArgs a) {
     const bool here = c < a.channels;
     const int64_t cb = (int64_t)(here ? c : 0) * Tok<BF>::BYTES;
 
-    if (blockIdx.x == 0) check_seqlens(a.cu, a.seqs, a.tokens, a.err, threadIdx.x, 256);
+    if (blockIdx.x == 0) {
+        check_seqlens(a.cu, a.seqs, a.tokens, a.err, threadIdx.x, 256);
+        // (slots of empty sequences, whose states nobody looks at below)
+        if (a.err && a.carry)
+            for (int b = threadIdx.x; b < a.seqs; b += 256) state_row(a.state, a.slots, b, a.n_slots, a.err);
+    }
     if (block >= a.blocks_t) {
         // empty sequences without carry: their state becomes zero
         if (a.carry) return;

@@ -236,3 +236,22 @@ def test_conv_of_no_tokens_reports_lengths_that_claim_some(carry):
             assert B.leapquant_check_error_word(err) == bits
             if st is not None:
                 assert torch.equal(st.cpu(), state if carry else torch.zeros_like(state))
+
+
+@pytest.mark.parametrize("carry", [False, True])
+@pytest.mark.parametrize("lens", [[0, 4], [0, 0]], ids=str)
+def test_conv_reports_the_bad_slot_of_an_empty_sequence(lens, carry):
+    """As the scan does."""
+    cu, n = packed(lens)
+    x, w = rnd(1, max(n, 1), 64).cuda()[:n], rnd(2, 64, 4).cuda()
+    for slots, bits in (([1, 0], 0), ([-1, 0], 0), ([2, 0], B.LQ_DEVERR_BAD_SLOT)):
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+        B.leapquant_conv_prompt(x, w, torch.empty_like(x), cu.cuda(), state=rnd(3, 2, 3, 64).cuda(), carry=carry,
+                                slots=torch.tensor(slots, dtype=torch.int32, device="cuda"), err=err)
+        assert B.leapquant_check_error_word(err) == bits
+        y = cu_args(scan_inputs(max(n, 1), 1, 1, BF))
+        tokens = [y[a][:n] for a in ("q", "k", "v", "dt")]
+        B.leapquant_scan_prompt(B.make_dims(2, 1, 1, rule=B.LQ_RULE_ADD), *tokens, y["A"], torch.empty_like(tokens[2]), cu.cuda(),
+                                state=torch.zeros((2, 1, 128, 128), device="cuda"), carry=carry,
+                                slots=torch.tensor(slots, dtype=torch.int32, device="cuda"), err=err)
+        assert B.leapquant_check_error_word(err) == bits
