@@ -256,8 +256,8 @@ ConvArgs conv_args(const lq_conv &c) {
     a.slots = c.slots;
     a.err = c.err;
     a.tokens = c.tokens;
-    a.x_stride = c.x_stride * (c.dtype == LQ_TOKEN_BF16 ? 2 : 4);
-    a.out_stride = c.out_stride * (c.out_dtype == LQ_TOKEN_BF16 ? 2 : 4);
+    a.x_stride = row_bytes(c.tokens, c.x_stride, c.dtype == LQ_TOKEN_BF16 ? 2 : 4);
+    a.out_stride = row_bytes(c.tokens, c.out_stride, c.out_dtype == LQ_TOKEN_BF16 ? 2 : 4);
     a.seqs = c.seqs;
     a.channels = c.channels;
     a.n_slots = c.n_slots;

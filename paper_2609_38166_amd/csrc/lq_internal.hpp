@@ -53,6 +53,9 @@ hipError_t launch_scan_prompt(const lq_dims &d, const lq_scan &s, hipStream_t st
 hipError_t launch_scan_step(const lq_dims &d, const lq_scan &s, hipStream_t st);
 hipError_t launch_scan_gates(const lq_dims &d, const lq_scan &s, float *alpha, float *beta, hipStream_t st);
 
+// Bytes between the rows of a token array; of one row's, nobody has to set a stride.
+inline int64_t row_bytes(int64_t tokens, int64_t stride, int64_t size) { return tokens > 1 ? stride * size : 0; }
+
 // host checks shared by the C ABI's source files (lq_api.hip)
 int32_t check_dims(const lq_dims *d);
 int32_t hip_status(hipError_t e);

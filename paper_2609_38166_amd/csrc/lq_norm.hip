@@ -152,10 +152,11 @@ hipError_t launch_qk_norm(const lq_qk &n, hipStream_t st) {
     a.sin = n.sin;
     a.positions = n.positions;
     a.err = n.err;
-    a.in_stride[0] = n.q_stride * es;
-    a.in_stride[1] = n.k_stride * es;
-    a.out_stride[0] = n.q_out_stride * eo;
-    a.out_stride[1] = n.k_out_stride * eo;
+    const int64_t rows_k = n.heads_k ? n.tokens : 0;
+    a.in_stride[0] = row_bytes(n.tokens, n.q_stride, es);
+    a.in_stride[1] = row_bytes(rows_k, n.k_stride, es);
+    a.out_stride[0] = row_bytes(n.tokens, n.q_out_stride, eo);
+    a.out_stride[1] = row_bytes(rows_k, n.k_out_stride, eo);
     a.heads_q = n.heads_q;
     a.heads = n.heads_q + n.heads_k;
     a.rows = n.tokens * a.heads;

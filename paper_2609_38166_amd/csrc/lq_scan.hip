@@ -877,11 +877,11 @@ ScanArgs scan_args(const lq_dims &d, const lq_scan &s) {
     a.slots = s.slots;
     a.err = s.err;
     a.tokens = s.tokens;
-    a.q_stride = s.q_stride * es;
-    a.k_stride = s.k_stride * es;
-    a.v_stride = s.v_stride * es;
-    a.dt_stride = s.dt_stride * es;
-    a.o_stride = s.o_stride * es;
+    a.q_stride = row_bytes(s.tokens, s.q_stride, es);
+    a.k_stride = row_bytes(s.tokens, s.k_stride, es);
+    a.v_stride = row_bytes(s.tokens, s.v_stride, es);
+    a.dt_stride = row_bytes(s.tokens, s.dt_stride, es);
+    a.o_stride = row_bytes(s.tokens, s.o_stride, es);
     a.batch = d.batch;
     a.heads_v = d.heads_v;
     a.group = d.heads_v / d.heads_k;
@@ -941,7 +941,7 @@ hipError_t launch_prompt(const lq_dims &d, const lq_scan &s, hipStream_t st) {
     p.length = sp.length;
     p.segments = (int32_t)sp.segments;
     p.parts = (float *)s.workspace;
-    p.decays = p.parts + sp.segments * d.heads_v * D * D;
+    p.decays = sp.length ? p.parts + sp.segments * d.heads_v * D * D : nullptr;      // (not cut: no workspace)
     const int64_t groups = (sp.segments * d.heads_k + 7) / 8 * 8;
     const dim3 grid((unsigned)(groups * p.s.group));
     if (!sp.length) {
