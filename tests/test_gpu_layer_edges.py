@@ -255,3 +255,40 @@ def test_conv_reports_the_bad_slot_of_an_empty_sequence(lens, carry):
                                 state=torch.zeros((2, 1, 128, 128), device="cuda"), carry=carry,
                                 slots=torch.tensor(slots, dtype=torch.int32, device="cuda"), err=err)
         assert B.leapquant_check_error_word(err) == bits
+
+
+def in_terms(x, n):
+    """The sum of n bf16 terms cut one after the other from fp32 values, the last one rounded."""
+    x, out = x.clone(), torch.zeros_like(x, dtype=torch.float64)
+    for i in range(n):
+        term = (x.view(torch.int32) & -65536).view(torch.float32) if i < n - 1 else x.bfloat16().float()
+        out, x = out + term.double(), x - term
+    return out
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lens", [[1], [5, 1], [40], [700]], ids=str)
+def test_scan_state_is_fp32(lens, dtype):
+    """No decay, and values in at most three tokens: few roundings, so that a state of fewer bits than fp32's shows.  A sum of
+    three products of a step, a key and a value: 4 roundings of each, 2 of the sum, and the step's own (softplus to 4 u)."""
+    cu, n = packed(lens)
+    seqs, hv = len(lens), 2
+    x = scan_inputs(n, hv, 1, dtype)
+    x["A"].zero_()
+    keep = torch.zeros(n, dtype=torch.bool)
+    keep[[0, n // 2, n - 1]] = True
+    x["v"][~keep] = 0
+    want, osize, new, size = R.scan(x["q"], x["k"], x["v"], x["dt"], x["A"], R.lengths(cu, n), x["D"], x["dt_bias"])
+    tol = 16 * U * size
+    raw = x["dt"].double() + x["dt_bias"].double()
+    wv = ((torch.clamp(raw, min=0) + torch.log1p(torch.exp(-raw.abs())))[:, :, None] * x["v"].double()).float()
+    for terms, enough in ((2, False), (3, True)):         # what a state from two terms of 16 bits would miss
+        ks = x["k"].double().repeat_interleave(hv, 1)
+        state = torch.stack([(in_terms(wv, terms)[lo:hi, :, :, None] * ks[lo:hi, :, None, :]).sum(0) for lo, hi in R.lengths(cu, n)])
+        assert bool(((state - new).abs() <= tol).all()) == enough
+    d = B.make_dims(seqs, hv, 1, rule=B.LQ_RULE_ADD)
+    assert (B.leapquant_scan_workspace_bytes(d, n, dtype, max(lens)) > 0) == (max(lens) == 700)
+    st = torch.empty((seqs, hv, 128, 128), device="cuda")
+    o = run_prompt(d, x, cu, n, dtype, st, max_len=max(lens))
+    close(st, new, tol)
+    close(o, want, fp32_tolerance(osize, max(lens)))
