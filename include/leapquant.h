@@ -439,7 +439,8 @@ int32_t leapquant_scan_workspace_bytes(const lq_dims *dims, const lq_scan *s, si
 /* leapquant_scan_prompt -- all tokens of packed sequences, fp32 states.  Tokens and
  * states that are not finite give NaN and infinities where the recurrence does (NaN
  * makes a (sequence, head) some 3 times slower, an infinity some 10 times).  A decay
- * over several tokens counts as above zero however small. */
+ * over several tokens counts as above zero however small; after one that is infinite (a
+ * step of -inf without softplus) a long prompt's results may be NaN in an infinity's place. */
 int32_t leapquant_scan_prompt(const lq_dims *dims, const lq_scan *s, void *stream);
 
 /* leapquant_scan_step -- one token of every request (row b of the token

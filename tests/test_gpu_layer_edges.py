@@ -292,3 +292,26 @@ def test_scan_state_is_fp32(lens, dtype):
     o = run_prompt(d, x, cu, n, dtype, st, max_len=max(lens))
     close(st, new, tol)
     close(o, want, fp32_tolerance(osize, max(lens)))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [16, 300], ids=["one chunk", "split"])
+def test_scan_decays_keep_their_bits_where_they_are_strong(n, dtype):
+    """A state without new values, steps that are exact: each chunk (of at least 16 tokens) or segment multiplies it by one
+    power of two, good to 2 u of the exponential, 1 u of its argument and 1 u of the product, however strong the decay."""
+    x = scan_inputs(n, 2, 2, dtype)
+    x["v"].zero_()
+    x["q"].zero_()
+    x["q"][..., 9] = 1
+    x["dt"] = (0.75 + 0.25 * torch.rand((n, 2), generator=torch.Generator().manual_seed(1))).to(dtype)
+    x["A"] = torch.tensor([-0.301, -3.1]) if n == 16 else torch.tensor([-0.011, -0.25])
+    x["dt_bias"] = x["D"] = None
+    state = rnd(9, 1, 2, 128, 128)
+    want, osize, new, size = R.scan(x["q"], x["k"], x["v"], x["dt"], x["A"], [(0, n)], None, None, False, state)
+    d = B.make_dims(1, 2, 2, rule=B.LQ_RULE_ADD)
+    assert (B.leapquant_scan_workspace_bytes(d, n, dtype, n) > 0) == (n == 300)
+    st = state.cuda()
+    o = run_prompt(d, x, torch.tensor([0, n], dtype=torch.int32), n, dtype, st, True, None, n, softplus=False)
+    factors = 1 if n == 16 else -(-n // 64) + 64 // 16    # a segment's start is a product over segments, then chunks follow
+    close(st, new, 4 * U * factors * size)
+    close(o, want, 4 * U * (factors + 1) * osize)
