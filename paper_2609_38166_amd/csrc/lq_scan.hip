@@ -238,9 +238,9 @@ __device__ __forceinline__ bf16x8 frag_turned(uint32_t at) {
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 // 2^x with the rounding of a small exponent only (x rounded to fp32 as it is puts |x| ln 2
 // half ulps on the result): for what a whole state is multiplied with.  (The weights of single
-// tokens do without: where x is large, the weight is small beside the others.)
+// tokens do without: where x is large, the weight is small beside the others.)  x = inf gives
+// NaN.
 __device__ __forceinline__ float exp2_wide(double x) {
-    x = x > 1000.0 ? 1000.0 : x;                          // (inf - inf below; 2^1000 is infinite here)
     const double n = __builtin_rint(x);
     return ldexpf(exp2_hw((float)(x - n)), (int)n);
 }
@@ -816,7 +816,7 @@ __global__ __launch_bounds__(256, !BF && MODE == PARTS ? 4 : 3) void scan_prompt
         wait_vm_all();                          // outputs and state are stored
         walk_by_token<BF, MODE>(args->s, begin, end, h, wave, again, start, keeps ? Sp : nullptr);
     }
-    if (MODE == PARTS && tid == 0) p.decays[(int64_t)seg * a.heads_v + h] = exp2_wide(total);
+    if (MODE == PARTS && tid == 0) p.decays[(int64_t)seg * a.heads_v + h] = exp2_wide(total > 1000.0 ? 1000.0 : total);
 }
 
 // Start states of the segments from their own sums, and the final state: per
