@@ -775,12 +775,15 @@ __global__ __launch_bounds__(256, !BF && MODE == PARTS ? 4 : 3) void scan_prompt
     }
 
     if (MODE != OUTPUT) {
+        f32x4 sum[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};     // (eight chains, not one)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) odd_sum = fmaf(S[i][u][r], 0.0f, odd_sum);
+                for (int r = 0; r < 4; ++r) sum[u][r] = fmaf(S[i][u][r], 0.0f, sum[u][r]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) odd_sum += sum[0][r] + sum[1][r];
     }
     int again = lane;                           // (the first load's addresses would stay in registers all along)
     asm volatile("" : "+v"(again));
