@@ -5,7 +5,7 @@
 // channels of a run of tokens, whose input rows it reads once into registers;
 // neighbouring lanes own neighbouring channels, so every access is whole lines.
 // 8192 tokens x 8192 channels, bf16, K = 4: 62 us (a large copy's rate: 56); a wave that
-// walks one run only 66.6.  256 tokens x 12288 channels 12.1 us (11.9).
+// walks one run only 65-70.  256 tokens x 12288 channels 12.1 us (11.9).
 #include <algorithm>
 
 #include "lq_layer.hpp"
@@ -284,10 +284,12 @@ hipError_t launch(ConvArgs a, bool step, hipStream_t st) {
             hipLaunchKernelGGL((conv_step_kernel<K, BF, OBF, 1>), dim3((unsigned)single), dim3(256), 0, st, a);
     } else {
         // Runs per wave: as few as leave one round of workgroups (512: their registers allow
-        // two per CU), up to eight; a launch of several rounds anyway takes two.  Measured:
-        // 131 tokens x 1536 fp32 channels 6.3 us with one, 14.4 with eight; 8192 x 8192 bf16
-        // 71, 66, 69, 63, 75 us with 1, 2, 4, 8, 16 (eight: exactly one round); 32768 x
-        // 12288 bf16 306 us with two, 310 with eight.
+        // two per CU), up to eight; a launch of several rounds anyway takes two.  us, each
+        // timed by itself in one go: 131 tokens x 1536 fp32 channels 5.3, 6.5, 14.0 with 1, 2, 8;
+        // 2048 x 8192 bf16 20, 17, 19, 20 with 1, 2 (the rule's), 3, 4; 3000 x 6144 bf16 22, 21, 19,
+        // 22, 26 with 1, 2, 3 (the rule's), 4, 8; 8192 x 8192 bf16 65, 59, 60, 62, 62, 61, 67, 57
+        // with 1 .. 8 (eight: exactly one round), 75 with 16; 32768 x 12288 bf16 354, 304, 302,
+        // 309 with 1, 2, 4, 8.  Not so good: 4096 x 8192 fp32 51, 60, 53, 56, 57, 57, 59, 61 with 1 .. 8.
         const int64_t groups = (a.tokens + 4 * RUN - 1) / (4 * RUN), round = std::max(512 / a.blocks_c, 1);
         const int64_t runs = std::max<int64_t>((groups + round - 1) / round, 1);
         a.runs = runs > 8 ? 2 : (int)runs;

@@ -33,7 +33,7 @@ __device__ __forceinline__ void load8(const char *p, float *f) {
 // Bound: HBM, the state read and written once.  M rows of S^T per thread, 8 key
 // channels each: 16 lanes hold a row, so the output's sum is a DPP row sum, and a
 // workgroup holds 16 M rows, 8 / M workgroups a tile.  256 requests x 32 heads, fp32
-// state: 188 us (5.8 TB/s) with one row a thread, 220 with eight.
+// state: 188 us (5.8 TB/s) with one row a thread, 215 with eight.
 template <bool BF, bool SBF, int M>
 __global__ __launch_bounds__(NT) void scan_step_kernel(ScanArgs a) {
     constexpr int PARTS = 8 / M, SB = SBF ? 2 : 4;
@@ -114,12 +114,12 @@ __global__ __launch_bounds__(NT) void scan_step_kernel(ScanArgs a) {
 // bf16 tokens are exact operands.  What is multiplied with them in fp32 (the
 // state, P, w v) is split into three bf16 terms, which hold all its 24 bits: sums are
 // those of fp32 also where they cancel.  (Two terms for the outputs are a tenth faster,
-// 64 ragged prompts 180 instead of 203 us, but drop what lies below 2^-16 of a term.)
+// 64 ragged prompts 180 instead of 203 us when the third came, but drop what lies below 2^-16 of a term.)
 // fp32 tokens go through the fp32 matrix instructions.
 //
 // Bound: bf16, the issue of matrix and vector instructions, which do not overlap, beside
-// HBM; fp32, the matrix cores (64% busy in the output pass).  64 ragged prompts, 16383
-// tokens x 32 heads: 203 us; one of 32768 x 16 heads 257; 2048 fp32 tokens x 32 heads 98.
+// HBM; fp32, the matrix cores (63% busy in the output pass).  64 ragged prompts, 16383
+// tokens x 32 heads: 205 us; one of 32768 x 16 heads 259; 2048 fp32 tokens x 32 heads 99.
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -160,7 +160,8 @@ template <bool BF> struct Chunk {
     // transposing read (rows 4 r ..) or a column read of fp32 (rows r, r + 4, ..)
     // takes at once.  The counters show no conflicts for fp32, but 0.41 of the LDS's
     // active cycles for bf16, whose reads are not served in runs of 16 lanes; placements
-    // with 64% fewer took the same time (64 ragged prompts x 32 heads 182-186 us).
+    // with 64% fewer took the same time (64 ragged prompts x 32 heads 182-186 us, outputs from
+    // two terms).
     __device__ static __forceinline__ int place(int row, int piece) {
         return piece ^ (BF ? 4 * (row & 3) + ((row >> 2) & 3) : row & 15);
     }
@@ -902,16 +903,16 @@ ScanArgs scan_args(const lq_dims &d, const lq_scan &s) {
     return a;
 }
 
-// How a prompt's work is split.  A sequence's chunks follow one another (2.4 us a chunk of
-// 32 bf16 or 3.6 us of 16 fp32 tokens where a CU has one workgroup), so a launch has one
+// How a prompt's work is split.  A sequence's chunks follow one another (2.9 us a chunk of
+// 32 bf16 or 3.5 us of 16 fp32 tokens where a CU has one workgroup), so a launch has one
 // workgroup per (sequence, head) unless the sequences are cut into segments, which costs a
 // second pass over keys and values and the segments' states (64 KiB each, written, joined
 // and read).  They are cut so that the launch has two workgroups per CU, and only where a
 // segment is a small part of the longest sequence.  us without -> with, heads x tokens:
-// bf16 16 x 512 43 -> 29, 16 x 320 29 -> 25, 16 x 256 (64 a segment) 24 -> 24, of four
-// sequences 25 -> 31, 32 x 8192 566 -> 123; fp32 32 x 512 114 -> 50, 16 x 224 53 -> 38.
-// Three workgroups' worth instead of two: 32 x 8192 132, 16 x 32768 237 instead of 232;
-// one: 141, 268.
+// bf16 16 x 512 50 -> 30, 16 x 320 33 -> 26, 16 x 256 (64 a segment) 28 -> 25, of four
+// sequences 29 -> 33, 32 x 8192 729 -> 151; fp32 32 x 512 121 -> 53, 16 x 224 56 -> 40.
+// Three workgroups' worth instead of two: 32 x 8192 147 instead of 151, 16 x 32768 260 instead
+// of 259, fp32 32 x 2048 99 instead of 105; one: 158, 286, 107.
 struct Split {
     int32_t length;         // tokens of a segment; 0: not cut
     int64_t segments;
@@ -972,8 +973,8 @@ template <bool BF, bool SBF>
 hipError_t launch_step(const lq_dims &d, const lq_scan &s, hipStream_t st) {
     const ScanArgs a = scan_args(d, s);
     const int tiles = d.batch * d.heads_v;
-    // Rows per thread, us a call (1, 2, 4, 8): fp32 8192 tiles 185, 201, 203, 212; 2048 51, 52,
-    // 54, 59; 512 14.8, 13.4, 13.8, 14.0; bf16 8192 123, 101, 104, 115; 16 4.2, 4.2, 4.6, 5.0.
+    // Rows per thread, us a call (1, 2, 4, 8): fp32 8192 tiles 186, 201, 206, 215; 2048 49, 51,
+    // 53, 58; 512 14.5, 13.0, 13.4, 13.7; bf16 8192 123, 101, 104, 115; 16 4.2, 4.2, 4.6, 5.0.
     if constexpr (!SBF) {
         if (tiles >= 2048) {
             hipLaunchKernelGGL((scan_step_kernel<BF, SBF, 1>), dim3(8 * tiles), dim3(NT), 0, st, a);
