@@ -453,6 +453,128 @@ int32_t leapquant_scan_step(const lq_dims *dims, const lq_scan *s, void *stream)
  * LQ_RULE_ADD.  Reads tokens, dtype, softplus, dt, dt_stride, A and dt_bias. */
 int32_t leapquant_scan_gates(const lq_dims *dims, const lq_scan *s, float *alpha, float *beta, void *stream);
 
+/*
+ * ---- projection operators: a layer's rows and weights in 8 bits -------------
+ *
+ * What stands between a layer's hidden rows and the operators above: the
+ * residual's addition and the norm of hidden rows, the norm and the gate of the
+ * layer's outputs, and the products with its weights, in OCP E4M3 with a scale
+ * for each block of 128.  The conventions of the layer operators hold (rows at
+ * any distance that start at multiples of 16 bytes, fp32 parameters, arithmetic
+ * in fp32 or wider).
+ *
+ * E4M3 rows: a row of channels has a scale for each 128 of them (the last block
+ * may be shorter).  With most = max |y| over the block, at least 2^-100,
+ *   scale = most / 448,   code = e4m3(y * (448 / most)), to nearest even,
+ * and code * scale is what the row stands for.  A NaN in a block makes its scale
+ * and all its codes NaN; an infinity makes its scale infinite, its own code NaN
+ * and the others 0.  Scales are fp32 rows, `scale_stride` elements apart.
+ */
+#define LQ_TOKEN_E4M3 2      /* an output of leapquant_add_norm and leapquant_gate_norm */
+#define LQ_ACT_SILU    0     /* z / (1 + exp(-z))                                    */
+#define LQ_ACT_SIGMOID 1     /* 1 / (1 + exp(-z))                                    */
+#define LQ_SCALE_BLOCK 128
+#define LQ_MAX_NORM_CHANNELS 32768
+
+/*
+ * leapquant_add_norm -- h = x + residual, residual_out = h, and
+ *   out = h / sqrt(mean h^2 + eps) * weight  (LQ_NORM_RMS)  or  out = h  (LQ_NORM_NONE)
+ * of rows of channels, rounded once each (the norm reads h in fp32, not as
+ * residual_out holds it).  Without a residual h = x.  channels is a multiple of
+ * 8, at most LQ_MAX_NORM_CHANNELS.  residual_out may be residual (in place), and
+ * either output may be x, if the types and strides are the same.
+ */
+typedef struct {
+    int64_t tokens;
+    int32_t channels;
+    int32_t norm;               /* LQ_NORM_NONE or LQ_NORM_RMS                      */
+    int32_t dtype;              /* x: LQ_TOKEN_F32 or _BF16                         */
+    int32_t residual_dtype;     /* residual and residual_out: the same choice       */
+    int32_t out_dtype;          /* LQ_TOKEN_F32, _BF16 or _E4M3                     */
+    float eps;
+    int64_t x_stride, residual_stride, residual_out_stride, out_stride, scale_stride;
+    const void *x;              /* [tokens][channels]                               */
+    const void *residual;       /* [tokens][channels] or NULL (none)                */
+    const float *weight;        /* [channels] or NULL (ones); LQ_NORM_RMS only      */
+    void *residual_out;         /* [tokens][channels] or NULL (not kept)            */
+    void *out;                  /* [tokens][channels]                               */
+    float *scale;               /* [tokens][ceil(channels / 128)], E4M3 only        */
+} lq_add;
+int32_t leapquant_add_norm(const lq_add *a, void *stream);
+
+/*
+ * leapquant_gate_norm -- RMS norm of every head of the layer's outputs, times its
+ * gate: with a = act(gate),
+ *   out = x / sqrt(mean x^2 + eps) * weight * a,  or, gate_first,
+ *   out = x a / sqrt(mean (x a)^2 + eps) * weight.
+ * d, the channels under one norm, is 64 or a multiple of 128 up to
+ * LQ_MAX_NORM_CHANNELS.  The blocks of an E4M3 output run over the token's row of
+ * heads * d channels.  out may be x or gate (same type and stride).
+ */
+typedef struct {
+    int64_t tokens;
+    int32_t heads, d;
+    int32_t act;                /* LQ_ACT_*                                         */
+    int32_t gate_first;         /* 1: the norm reads the gated values               */
+    int32_t weight_heads;       /* 1: a weight per head, [heads][d]; 0: one, [d]    */
+    int32_t dtype, gate_dtype;  /* x, gate: LQ_TOKEN_F32 or _BF16                   */
+    int32_t out_dtype;          /* LQ_TOKEN_F32, _BF16 or _E4M3                     */
+    float eps;
+    int64_t x_stride, gate_stride, out_stride, scale_stride;
+    const void *x, *gate;       /* [tokens][heads][d]                               */
+    const float *weight;        /* [d] or [heads][d], or NULL (ones)                */
+    void *out;                  /* [tokens][heads][d]                               */
+    float *scale;               /* [tokens][ceil(heads * d / 128)], E4M3 only       */
+} lq_gated;
+int32_t leapquant_gate_norm(const lq_gated *g, void *stream);
+
+/*
+ * leapquant_quantize_weight -- a weight [n][k] in E4M3 with a scale for each block
+ * of 128 x 128, by the rule above with the largest magnitude of the whole block.
+ * k is a multiple of 16.
+ */
+typedef struct {
+    int32_t n, k;
+    int32_t dtype;              /* w: LQ_TOKEN_F32 or _BF16                         */
+    int64_t w_stride, out_stride;
+    const void *w;              /* [n][k]                                           */
+    void *out;                  /* [n][k] E4M3                                      */
+    float *scale;               /* [ceil(n / 128)][ceil(k / 128)], dense            */
+} lq_weight;
+int32_t leapquant_quantize_weight(const lq_weight *w, void *stream);
+
+/*
+ * leapquant_matmul -- product of E4M3 rows and an E4M3 weight:
+ *   out[t][i] = bias[i] + sum_b x_scale[t][b] w_scale[i / 128][b] sum_{j in b} x[t][j] w[i][j],
+ * sums in fp32, rounded once.  fp32 outputs are the sums of exact products.  bf16
+ * outputs come from the matrix cores' 8-bit products, which keep of every 8 products
+ * the bits above 2^-13 of the largest: a sum is off by about 1.4e-5 of the sums' size
+ * beside its rounding, at most 7 * 2^-13 of its terms where it cancels (take fp32
+ * outputs where that matters; they run at about half the rate).  k is a multiple of
+ * 16, n any; rows of x and w are at most 2^23 elements apart.  Large weights on few tokens are split over k and need
+ * a workspace (leapquant_matmul_workspace_bytes, often 0); results do not depend
+ * on where it lies, and the order of sums is the same in every call of the same sizes.
+ */
+typedef struct {
+    int64_t tokens;
+    int32_t n, k;
+    int32_t out_dtype;          /* LQ_TOKEN_F32 or _BF16                            */
+    int64_t x_stride, x_scale_stride, w_stride, out_stride;
+    const void *x;              /* [tokens][k] E4M3                                 */
+    const float *x_scale;       /* [tokens][ceil(k / 128)]                          */
+    const void *w;              /* [n][k] E4M3                                      */
+    const float *w_scale;       /* [ceil(n / 128)][ceil(k / 128)], dense            */
+    const float *bias;          /* [n] or NULL (0)                                  */
+    void *out;                  /* [tokens][n]                                      */
+    void *workspace;            /* 16-byte aligned device memory, overwritten       */
+    size_t workspace_bytes;
+} lq_matmul;
+int32_t leapquant_matmul(const lq_matmul *m, void *stream);
+
+/* leapquant_matmul_workspace_bytes -- host only: workspace (may be 0) that
+ * leapquant_matmul needs for these tokens, n, k and out_dtype. */
+int32_t leapquant_matmul_workspace_bytes(const lq_matmul *m, size_t *bytes_out);
+
 /* Static description of a status code. */
 const char *leapquant_strerror(int32_t status);
 

@@ -29,6 +29,9 @@ LQ_DEVERR_BAD_REC_LEN = 2
 LQ_DEVERR_BAD_SEQLENS, LQ_DEVERR_BAD_SLOT, LQ_DEVERR_BAD_POSITION = 4, 8, 16
 LQ_TOKEN_F32, LQ_TOKEN_BF16 = 0, 1
 LQ_NORM_NONE, LQ_NORM_L2, LQ_NORM_RMS = 0, 1, 2
+LQ_TOKEN_E4M3 = 2
+LQ_ACT_SILU, LQ_ACT_SIGMOID = 0, 1
+LQ_SCALE_BLOCK = 128
 
 EXPORTS = ("leapquant_state_bytes", "leapquant_quantize_state", "leapquant_decode_step",
            "leapquant_decode_step_general", "leapquant_decode_step_commit", "leapquant_window_commit",
@@ -36,7 +39,9 @@ EXPORTS = ("leapquant_state_bytes", "leapquant_quantize_state", "leapquant_decod
            "leapquant_baseline_step_general", "leapquant_dequantize_state",
            "leapquant_check_error", "leapquant_strerror", "leapquant_last_hip_error",
            "leapquant_conv_prompt", "leapquant_conv_step", "leapquant_qk_norm", "leapquant_scan_workspace_bytes",
-           "leapquant_scan_prompt", "leapquant_scan_step", "leapquant_scan_gates")
+           "leapquant_scan_prompt", "leapquant_scan_step", "leapquant_scan_gates",
+           "leapquant_add_norm", "leapquant_gate_norm", "leapquant_quantize_weight", "leapquant_matmul",
+           "leapquant_matmul_workspace_bytes")
 
 
 class LeapQuantError(RuntimeError):
@@ -76,6 +81,17 @@ lq_scan = _struct("lq_scan", (("l", "tokens"), ("i", "dtype state_dtype softplus
                               ("l", "q_stride k_stride v_stride dt_stride o_stride"),
                               ("p", "q k v dt A skip dt_bias o state cu_seqlens slots err workspace"),
                               ("z", "workspace_bytes")))
+# ... and the projection operators'
+lq_add = _struct("lq_add", (("l", "tokens"), ("i", "channels norm dtype residual_dtype out_dtype"), ("f", "eps"),
+                            ("l", "x_stride residual_stride residual_out_stride out_stride scale_stride"),
+                            ("p", "x residual weight residual_out out scale")))
+lq_gated = _struct("lq_gated", (("l", "tokens"), ("i", "heads d act gate_first weight_heads dtype gate_dtype out_dtype"),
+                                ("f", "eps"), ("l", "x_stride gate_stride out_stride scale_stride"),
+                                ("p", "x gate weight out scale")))
+lq_weight = _struct("lq_weight", (("i", "n k dtype"), ("l", "w_stride out_stride"), ("p", "w out scale")))
+lq_matmul = _struct("lq_matmul", (("l", "tokens"), ("i", "n k out_dtype"),
+                                  ("l", "x_stride x_scale_stride w_stride out_stride"),
+                                  ("p", "x x_scale w w_scale bias out workspace"), ("z", "workspace_bytes")))
 
 
 _L = None
@@ -84,7 +100,8 @@ _L = None
 _M = None
 _FN = {"leapquant_decode_step": 0, "leapquant_decode_step_general": 0, "leapquant_decode_step_commit": 0,
        "leapquant_window_commit": 0, "leapquant_conv_prompt": 0, "leapquant_conv_step": 0, "leapquant_qk_norm": 0,
-       "leapquant_scan_prompt": 0, "leapquant_scan_step": 0, "leapquant_scan_workspace_bytes": 0}
+       "leapquant_scan_prompt": 0, "leapquant_scan_step": 0, "leapquant_scan_workspace_bytes": 0, "leapquant_add_norm": 0,
+       "leapquant_gate_norm": 0, "leapquant_quantize_weight": 0, "leapquant_matmul": 0, "leapquant_matmul_workspace_bytes": 0}
 
 
 class _NoMarshal:
@@ -96,6 +113,7 @@ class _NoMarshal:
         return None
 
     step_general = commit = conv = qk_norm = scan = step
+    add_norm = gate_norm = quantize_weight = matmul = step
 
 
 def _load_marshal(addr):
@@ -139,6 +157,11 @@ def _lib():
         L.leapquant_scan_prompt.argtypes = [vp, vp, vp]
         L.leapquant_scan_step.argtypes = [vp, vp, vp]
         L.leapquant_scan_gates.argtypes = [vp, vp, vp, vp, vp]
+        L.leapquant_add_norm.argtypes = [vp, vp]
+        L.leapquant_gate_norm.argtypes = [vp, vp]
+        L.leapquant_quantize_weight.argtypes = [vp, vp]
+        L.leapquant_matmul.argtypes = [vp, vp]
+        L.leapquant_matmul_workspace_bytes.argtypes = [vp, vp]
         L.leapquant_strerror.argtypes = [i32]
         L.leapquant_strerror.restype = C.c_char_p
         L.leapquant_last_hip_error.argtypes = []
@@ -658,3 +681,145 @@ def leapquant_check_error_word(err, stream=None) -> int:
     if status not in (LQ_OK, LQ_EDEVICE):
         raise LeapQuantError(status, "leapquant_check_error")
     return bits.value
+
+
+# ---- projection operators: residual and norm, gated norm, weights and products in E4M3 ----
+
+_OUT = {**_TOKEN, torch.float8_e4m3fn: LQ_TOKEN_E4M3}
+E4M3 = torch.float8_e4m3fn
+
+
+def _out(t, name):
+    if t.dtype not in _OUT:
+        raise ValueError(f"{name} must be float32, bfloat16 or float8_e4m3fn, got {t.dtype}")
+    return _OUT[t.dtype]
+
+
+def _blocks(channels):
+    return -(-channels // LQ_SCALE_BLOCK)
+
+
+def _here(first, *others):
+    """All tensors on the current device, whose stream the call goes to."""
+    for t in (first, *others):
+        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor is on {t.device}, the current device is {torch.cuda.current_device()}")
+
+
+def _scales(scale, out, tokens, channels):
+    """Address and stride of an E4M3 output's scales (None for the other types)."""
+    if out.dtype != E4M3:
+        if scale is not None:
+            raise ValueError("scale belongs to a float8_e4m3fn output")
+        return None, 0
+    if scale is None:
+        raise ValueError("scale is required for a float8_e4m3fn output")
+    return _rows(scale, "scale", (tokens, _blocks(channels)), torch.float32)
+
+
+def leapquant_add_norm(x, out, residual=None, residual_out=None, weight=None, norm=LQ_NORM_RMS, eps=1e-6, scale=None,
+                       stream=None):
+    """h = x + residual (kept in residual_out) and its RMS norm times weight (or h itself, LQ_NORM_NONE), rows [tokens,
+    channels]; out fp32, bf16, or float8_e4m3fn with scale fp32 [tokens, ceil(channels / 128)].  residual_out may be
+    residual, in place."""
+    if stream is None and (_M or _lib()):
+        status = _M.add_norm(_FN["leapquant_add_norm"], x, out, residual, residual_out, weight, norm, eps, scale)
+        if status is not None:
+            return _check(status, "leapquant_add_norm")
+    if x.dim() != 2:
+        raise ValueError("x must be [tokens, channels]")
+    _here(x, out, residual, residual_out, weight, scale)
+    shape = tokens, channels = tuple(x.shape)
+    px, xs = _rows(x, "x", shape)
+    po, os_ = _rows(out, "out", shape)
+    pr = ps = None
+    rs = ss = 0
+    kind = x
+    if residual is not None:
+        pr, rs = _rows(residual, "residual", shape)
+        kind = residual
+    if residual_out is not None:
+        ps, ss = _rows(residual_out, "residual_out", shape, residual.dtype if residual is not None else None)
+        kind = residual_out
+    pc, cs = _scales(scale, out, tokens, channels)
+    a = lq_add(tokens, channels, norm, _token(x, "x"), _token(kind, "residual"), _out(out, "out"), eps, xs, rs, ss, os_, cs, px, pr,
+               _dense(weight, "weight", (channels,), optional=True), ps, po, pc)
+    _check(_lib().leapquant_add_norm(C.byref(a), _stream(stream)), "leapquant_add_norm")
+
+
+def leapquant_gate_norm(x, gate, out, weight=None, act=LQ_ACT_SILU, gate_first=False, eps=1e-6, scale=None, stream=None):
+    """RMS norm of every head of x [tokens, heads, d] times weight ([d] or [heads, d]) and act(gate) (gate_first: the norm of
+    x * act(gate) times weight); out fp32, bf16, or float8_e4m3fn with scale fp32 [tokens, ceil(heads * d / 128)]."""
+    if stream is None and (_M or _lib()):
+        status = _M.gate_norm(_FN["leapquant_gate_norm"], x, gate, out, weight, act, gate_first, eps, scale)
+        if status is not None:
+            return _check(status, "leapquant_gate_norm")
+    if x.dim() != 3:
+        raise ValueError("x must be [tokens, heads, d]")
+    _here(x, gate, out, weight, scale)
+    shape = tokens, heads, d = tuple(x.shape)
+    px, xs = _rows(x, "x", shape)
+    pg, gs = _rows(gate, "gate", shape)
+    po, os_ = _rows(out, "out", shape)
+    pc, cs = _scales(scale, out, tokens, heads * d)
+    each = weight is not None and weight.dim() == 2
+    pw = _dense(weight, "weight", (heads, d) if each else (d,), optional=True)
+    a = lq_gated(tokens, heads, d, act, int(gate_first), int(each), _token(x, "x"), _token(gate, "gate"), _out(out, "out"), eps, xs,
+                 gs, os_, cs, px, pg, pw, po, pc)
+    _check(_lib().leapquant_gate_norm(C.byref(a), _stream(stream)), "leapquant_gate_norm")
+
+
+def leapquant_quantize_weight(weight, out, scale, stream=None):
+    """A weight [n, k] (fp32 or bf16) in float8_e4m3fn, out [n, k], with scale fp32 [ceil(n / 128), ceil(k / 128)]."""
+    if stream is None and (_M or _lib()):
+        status = _M.quantize_weight(_FN["leapquant_quantize_weight"], weight, out, scale)
+        if status is not None:
+            return _check(status, "leapquant_quantize_weight")
+    if weight.dim() != 2:
+        raise ValueError("weight must be [n, k]")
+    _here(weight, out, scale)
+    shape = n, k = tuple(weight.shape)
+    pw, ws = _rows(weight, "weight", shape)
+    po, os_ = _rows(out, "out", shape, E4M3)
+    a = lq_weight(n, k, _token(weight, "weight"), ws, os_, pw, po, _dense(scale, "scale", (_blocks(n), _blocks(k))))
+    _check(_lib().leapquant_quantize_weight(C.byref(a), _stream(stream)), "leapquant_quantize_weight")
+
+
+def leapquant_matmul(x, x_scale, weight, weight_scale, out, bias=None, workspace=None, stream=None):
+    """out [tokens, n] (fp32 or bf16) = x [tokens, k] times weight [n, k] transposed, plus bias [n]: x float8_e4m3fn with x_scale
+    [tokens, ceil(k / 128)], weight float8_e4m3fn with weight_scale [ceil(n / 128), ceil(k / 128)].  The workspace, where
+    one is needed, is allocated here unless a uint8 tensor is given; a stream of the caller's needs one."""
+    if stream is None and (_M or _lib()):
+        status = _M.matmul(_FN["leapquant_matmul"], _FN["leapquant_matmul_workspace_bytes"], x, x_scale, weight, weight_scale, out,
+                           bias, workspace)
+        if status is not None:
+            return _check(status, "leapquant_matmul")
+    if x.dim() != 2 or weight.dim() != 2:
+        raise ValueError("x must be [tokens, k] and weight [n, k]")
+    _here(x, x_scale, weight, weight_scale, out, bias, workspace)
+    (tokens, k), n = x.shape, weight.shape[0]
+    px, xs = _rows(x, "x", (tokens, k), E4M3)
+    pxs, xss = _rows(x_scale, "x_scale", (tokens, _blocks(k)), torch.float32)
+    pw, ws = _rows(weight, "weight", (n, k), E4M3)
+    pws = _dense(weight_scale, "weight_scale", (_blocks(n), _blocks(k)))
+    po, os_ = _rows(out, "out", (tokens, n))
+    a = lq_matmul(tokens, n, k, _token(out, "out"), xs, xss, ws, os_, px, pxs, pw, pws, _dense(bias, "bias", (n,), optional=True), po,
+                  None, 0)
+    need = C.c_size_t(0)
+    _check(_lib().leapquant_matmul_workspace_bytes(C.byref(a), C.byref(need)), "leapquant_matmul_workspace_bytes")
+    if need.value:
+        if workspace is None:
+            if stream is not None:
+                raise ValueError(f"a call on a stream of the caller's needs a workspace of {need.value} bytes")
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+        a.workspace, a.workspace_bytes = _device(workspace, "workspace", torch.uint8), workspace.numel()
+        _need(workspace, need.value, "workspace")
+    _check(_lib().leapquant_matmul(C.byref(a), _stream(stream)), "leapquant_matmul")
+
+
+def leapquant_matmul_workspace_bytes(tokens, n, k, out_dtype=torch.bfloat16) -> int:
+    """Workspace that leapquant_matmul needs for these sizes."""
+    need = C.c_size_t(0)
+    a = lq_matmul(tokens=tokens, n=n, k=k, out_dtype=_TOKEN[out_dtype])
+    _check(_lib().leapquant_matmul_workspace_bytes(C.byref(a), C.byref(need)), "leapquant_matmul_workspace_bytes")
+    return need.value

@@ -53,6 +53,13 @@ hipError_t launch_scan_prompt(const lq_dims &d, const lq_scan &s, hipStream_t st
 hipError_t launch_scan_step(const lq_dims &d, const lq_scan &s, hipStream_t st);
 hipError_t launch_scan_gates(const lq_dims &d, const lq_scan &s, float *alpha, float *beta, hipStream_t st);
 
+// projection operators (checked before they get here, likewise)
+hipError_t launch_add_norm(const lq_add &a, hipStream_t st);
+hipError_t launch_gate_norm(const lq_gated &g, hipStream_t st);
+hipError_t launch_quantize_weight(const lq_weight &w, hipStream_t st);
+size_t matmul_workspace_bytes(const lq_matmul &m);
+hipError_t launch_matmul(const lq_matmul &m, hipStream_t st);
+
 // Bytes between the rows of a token array; of one row's, nobody has to set a stride.
 inline int64_t row_bytes(int64_t tokens, int64_t stride, int64_t size) { return tokens > 1 ? stride * size : 0; }
 

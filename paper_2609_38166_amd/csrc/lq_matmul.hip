@@ -1,0 +1,215 @@
+// Product of E4M3 rows (a scale for each 128 channels) and an E4M3 weight (a scale for each block of 128 x 128):
+//   out[t][i] = bias[i] + sum_b xs[t][b] ws[i / 128][b] sum_{j in b} x[t][j] w[i][j].
+//
+// A block's sum is made from zero and added to the running sum with its scales, in fp32.  Output channels are the rows of a
+// tile and tokens its columns, so a lane holds one token, whose scale is one number, and 4 neighbouring channels.  The order
+// of a block's 128 products is free: both operands take 16-byte pieces g and g + 4 of their row in lane group g.
+//
+// bf16 outputs: the matrix cores' 8-bit products, a block in one instruction (16x16x128).  It adds them in groups of 8 with
+// the bits above 2^-13 of the group's largest product only (measured: a product 2^14 below another of its group is lost, one
+// 2^13 below is kept whole; across groups sums are fp32).  On normal values the sums are off by 1.4e-5 of their size, a
+// hundredth of what rounding to bf16 leaves; where a sum cancels, up to 7 * 2^-13 of its terms.  fp32 outputs: codes are
+// turned to bf16, which is exact, and multiplied there at half the rate, with sums of 1e-8.
+#include <algorithm>
+
+#include "lq_e4m3.hpp"
+#include "lq_internal.hpp"
+
+namespace lq {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+struct ProductArgs {
+    const char *x, *w;
+    const float *xs, *ws, *bias;
+    char *out;
+    int64_t x_stride, w_stride, out_stride;     // bytes
+    int64_t xs_stride;                          // floats
+    int32_t tokens, n, k, blocks;               // blocks: of k
+    int32_t out_bf16;
+};
+
+// 32 codes of a row, pieces g and g + 4 of a block, as operands
+template <bool EXACT> struct Operand;
+template <> struct Operand<false> {
+    i32x8 v;
+    __device__ __forceinline__ void set(const uint4 &a, const uint4 &b) {
+        v = i32x8{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
+    }
+};
+template <> struct Operand<true> {
+    bf16x8 v[4];
+    __device__ __forceinline__ void set(const uint4 &a, const uint4 &b) {
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bf16x2_t two = j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i + j / 2], 1.0f, true)
+                                           : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * i + j / 2], 1.0f, false);
+                v[i][2 * j] = two[0];
+                v[i][2 * j + 1] = two[1];
+            }
+    }
+};
+// a tile's sum over one block
+__device__ __forceinline__ f32x4 block_product(const Operand<false> &w, const Operand<false> &x) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 block_product(const Operand<true> &w, const Operand<true> &x) {
+    f32x4 p = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v[i], x.v[i], p, 0, 0, 0);
+    return p;
+}
+
+// 4 neighbouring channels of a token, from channel c on (rows start at multiples of 16 bytes).
+__device__ __forceinline__ void store4(const ProductArgs &a, int t, int c, f32x4 v) {
+    if (t >= a.tokens || c >= a.n) return;
+    if (a.bias) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] += a.bias[min(c + r, a.n - 1)];
+    }
+    char *at = a.out + t * a.out_stride + (int64_t)c * (a.out_bf16 ? 2 : 4);
+    if (c + 4 <= a.n) {
+        const float f[4] = {v[0], v[1], v[2], v[3]};
+        if (a.out_bf16) store_tok<true, 4>(at, f);
+        else store_tok<false, 4>(at, f);
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < 3; ++r) {
+        if (c + r >= a.n) break;
+        if (a.out_bf16) ((uint16_t *)at)[r] = (uint16_t)pk_bf16(v[r], v[r]);
+        else ((float *)at)[r] = v[r];
+    }
+}
+
+// ---- few tokens -------------------------------------------------------------------
+//
+// Bound: HBM, the weight.  A workgroup owns 16 CT channels of 16 TT tokens; its waves take the blocks of k in turn, AHEAD
+// of them at a time, straight from memory into registers, and join their sums in LDS.
+template <bool EXACT, int TT, int CT, int WAVES, int AHEAD>
+__global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs a) {
+    __shared__ f32x4 parts[WAVES][TT * CT][64];
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c0 = blockIdx.x * 16 * CT, t0 = blockIdx.y * 16 * TT;
+    const char *wrow[CT], *xrow[TT];
+    const float *srow[TT];
+#pragma unroll
+    for (int i = 0; i < CT; ++i) wrow[i] = a.w + min(c0 + 16 * i + l16, a.n - 1) * a.w_stride;
+#pragma unroll
+    for (int j = 0; j < TT; ++j) {
+        const int t = min(t0 + 16 * j + l16, a.tokens - 1);
+        xrow[j] = a.x + t * a.x_stride;
+        srow[j] = a.xs + t * a.xs_stride;
+    }
+    f32x4 acc[CT][TT] = {};
+    struct Pieces {
+        uint4 w[CT][2], x[TT][2];
+        float ws[CT], s[TT];
+    };
+    // block b's pieces; past k (the end of a last block that is shorter) zeros
+    auto load = [&](Pieces &o, int b, bool whole) {
+        const int at = b * BLOCK + 16 * g;
+        auto pieces = [&](const char *row, uint4 *p) {
+            const uint4 none = make_uint4(0, 0, 0, 0);
+            p[0] = whole || at < a.k ? *(const uint4 *)(row + at) : none;
+            p[1] = whole || at + 64 < a.k ? *(const uint4 *)(row + at + 64) : none;
+        };
+#pragma unroll
+        for (int i = 0; i < CT; ++i) {
+            pieces(wrow[i], o.w[i]);
+            o.ws[i] = a.ws[min(c0 + 16 * i, a.n - 1) / BLOCK * a.blocks + b];
+        }
+#pragma unroll
+        for (int j = 0; j < TT; ++j) {
+            pieces(xrow[j], o.x[j]);
+            o.s[j] = srow[j][b];
+        }
+    };
+    auto add = [&](const Pieces &o) {
+        Operand<EXACT> w[CT];
+#pragma unroll
+        for (int i = 0; i < CT; ++i) w[i].set(o.w[i][0], o.w[i][1]);
+#pragma unroll
+        for (int j = 0; j < TT; ++j) {
+            Operand<EXACT> x;
+            x.set(o.x[j][0], o.x[j][1]);
+#pragma unroll
+            for (int i = 0; i < CT; ++i) {
+                const f32x4 p = block_product(w[i], x);
+                const float f = o.s[j] * o.ws[i];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(p[r], f, acc[i][j][r]);
+            }
+        }
+    };
+    const int whole = a.k / BLOCK;
+    int b = wave;
+    for (; b + (AHEAD - 1) * WAVES < whole; b += AHEAD * WAVES) {
+        Pieces o[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) load(o[u], b + u * WAVES, true);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) add(o[u]);
+    }
+    for (; b < a.blocks; b += WAVES) {
+        Pieces o;
+        load(o, b, b < whole);
+        add(o);
+    }
+#pragma unroll
+    for (int i = 0; i < CT; ++i)
+#pragma unroll
+        for (int j = 0; j < TT; ++j) parts[wave][i * TT + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int e = tid; e < TT * CT * 64; e += 64 * WAVES) {
+        const int tile = e >> 6, from = e & 63;
+        f32x4 v = parts[0][tile][from];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) v += parts[i][tile][from];
+        store4(a, t0 + 16 * (tile % TT) + (from & 15), c0 + 16 * (tile / TT) + 4 * (from >> 4), v);
+    }
+}
+
+template <int TT, int CT, int WAVES, int AHEAD>
+hipError_t launch_few(const ProductArgs &a, hipStream_t st) {
+    const dim3 grid((unsigned)((a.n - 1) / (16 * CT) + 1), (unsigned)((a.tokens - 1) / (16 * TT) + 1)), block(64 * WAVES);
+    if (a.out_bf16) hipLaunchKernelGGL((product_few_kernel<false, TT, CT, WAVES, AHEAD>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((product_few_kernel<true, TT, CT, WAVES, AHEAD>), grid, block, 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t matmul_workspace_bytes(const lq_matmul &) { return 0; }
+
+hipError_t launch_matmul(const lq_matmul &m, hipStream_t st) {
+    if (m.tokens == 0) return hipSuccess;
+    ProductArgs a;
+    a.x = (const char *)m.x;
+    a.w = (const char *)m.w;
+    a.xs = m.x_scale;
+    a.ws = m.w_scale;
+    a.bias = m.bias;
+    a.out = (char *)m.out;
+    a.x_stride = row_bytes(m.tokens, m.x_stride, 1);
+    a.xs_stride = row_bytes(m.tokens, m.x_scale_stride, 1);
+    a.w_stride = row_bytes(m.n, m.w_stride, 1);
+    a.out_stride = row_bytes(m.tokens, m.out_stride, m.out_dtype == LQ_TOKEN_BF16 ? 2 : 4);
+    a.tokens = (int32_t)m.tokens;
+    a.n = m.n;
+    a.k = m.k;
+    a.blocks = (m.k + BLOCK - 1) / BLOCK;
+    a.out_bf16 = m.out_dtype == LQ_TOKEN_BF16;
+    if (m.tokens <= 16) return launch_few<1, 1, 8, 4>(a, st);
+    return launch_few<4, 4, 4, 1>(a, st);
+}
+
+}  // namespace lq

@@ -419,6 +419,188 @@ PyObject *scan(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// ---- projection operators: the checks of the binding's leapquant_add_norm, _gate_norm, _quantize_weight and _matmul ----
+
+constexpr at::ScalarType E4M3 = at::ScalarType::Float8_e4m3fn;
+
+bool out_type(const at::Tensor &t, int32_t *type) {
+    if (t.scalar_type() == E4M3) *type = LQ_TOKEN_E4M3;
+    else return token_type(t, type);
+    return true;
+}
+
+int64_t blocks(int64_t channels) { return (channels + LQ_SCALE_BLOCK - 1) / LQ_SCALE_BLOCK; }
+
+// The scales of an E4M3 output; none for the other types.
+bool scales(PyObject *o, int32_t out_dtype, int64_t tokens, int64_t channels, float **p, int64_t *stride) {
+    if (out_dtype != LQ_TOKEN_E4M3) return o == Py_None;
+    const int64_t size[2] = {tokens, blocks(channels)};
+    const void *q;
+    const at::Tensor *t;
+    if (!token_rows(o, 2, size, &q, stride, &t) || t->scalar_type() != F) return false;
+    *p = (float *)q;
+    return true;
+}
+
+// Whether all tensors (None passes) are on the current device.
+bool here(PyObject *const *a, Py_ssize_t from, Py_ssize_t to) {
+    const int device = c10::hip::getCurrentHIPStream().device_index();
+    for (Py_ssize_t i = from; i < to; ++i)
+        if (THPVariable_CheckExact(a[i]) && THPVariable_Unpack(a[i]).get_device() != device) return false;
+    return true;
+}
+
+template <typename T>
+void enqueue(int32_t &status, PyObject *fn, const T &args) {
+    using Fn = int32_t (*)(const T *, void *);
+    const Fn f = (Fn)PyLong_AsVoidPtr(fn);
+    void *s = current_stream();
+    Py_BEGIN_ALLOW_THREADS
+    status = f(&args, s);
+    Py_END_ALLOW_THREADS
+}
+
+bool number(PyObject *o, int32_t *p) {
+    const long x = PyLong_AsLong(o);
+    if (PyErr_Occurred() || x < INT32_MIN || x > INT32_MAX) return false;
+    *p = (int32_t)x;
+    return true;
+}
+bool real(PyObject *o, float *p) {
+    *p = (float)PyFloat_AsDouble(o);
+    return !PyErr_Occurred();
+}
+
+// add_norm(fn, x, out, residual, residual_out, weight, norm, eps, scale)
+PyObject *add_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 9) Py_RETURN_NONE;
+    return guarded([&](int32_t &status) {
+        lq_add c = {};
+        const at::Tensor *x, *t, *r;
+        const void *p;
+        void *v;
+        if (!device(a[1], false, &x, &v) || x->dim() != 2 || !here(a, 1, 9)) return false;
+        const int64_t size[2] = {x->size(0), x->size(1)};
+        if (size[1] > INT32_MAX) return false;
+        if (!token_rows(a[1], 2, size, &c.x, &c.x_stride, &x) || !token_type(*x, &c.dtype)) return false;
+        if (!token_rows(a[2], 2, size, &p, &c.out_stride, &t) || !out_type(*t, &c.out_dtype)) return false;
+        c.out = (void *)p;
+        c.residual_dtype = c.dtype;
+        if (a[3] != Py_None) {
+            if (!token_rows(a[3], 2, size, &c.residual, &c.residual_stride, &r) || !token_type(*r, &c.residual_dtype)) return false;
+        }
+        if (a[4] != Py_None) {
+            if (!token_rows(a[4], 2, size, &p, &c.residual_out_stride, &t)) return false;
+            if (a[3] != Py_None && t->scalar_type() != r->scalar_type()) return false;
+            if (!token_type(*t, &c.residual_dtype)) return false;
+            c.residual_out = (void *)p;
+        }
+        if (!vec(a[5], size[1], F, true, &c.weight) || !number(a[6], &c.norm) || !real(a[7], &c.eps)) return false;
+        if (!scales(a[8], c.out_dtype, size[0], size[1], &c.scale, &c.scale_stride)) return false;
+        c.tokens = size[0];
+        c.channels = (int32_t)size[1];
+        enqueue(status, a[0], c);
+        return true;
+    });
+}
+
+// gate_norm(fn, x, gate, out, weight, act, gate_first, eps, scale)
+PyObject *gate_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 9) Py_RETURN_NONE;
+    return guarded([&](int32_t &status) {
+        lq_gated c = {};
+        const at::Tensor *x, *t;
+        const void *p;
+        void *v;
+        if (!device(a[1], false, &x, &v) || x->dim() != 3 || !here(a, 1, 9)) return false;
+        const int64_t size[3] = {x->size(0), x->size(1), x->size(2)};
+        if (size[1] > INT32_MAX || size[2] > INT32_MAX) return false;
+        if (!token_rows(a[1], 3, size, &c.x, &c.x_stride, &x) || !token_type(*x, &c.dtype)) return false;
+        if (!token_rows(a[2], 3, size, &c.gate, &c.gate_stride, &t) || !token_type(*t, &c.gate_dtype)) return false;
+        if (!token_rows(a[3], 3, size, &p, &c.out_stride, &t) || !out_type(*t, &c.out_dtype)) return false;
+        c.out = (void *)p;
+        if (!device(a[4], true, &t, &v)) return false;
+        if (t) {
+            c.weight_heads = t->dim() == 2;
+            if (c.weight_heads ? !dense(a[4], 2, size + 1, F, false, &v) : !vec(a[4], size[2], F, false, &c.weight)) return false;
+            c.weight = (const float *)v;
+        }
+        if (!number(a[5], &c.act) || !flag(a[6], &c.gate_first) || !real(a[7], &c.eps)) return false;
+        if (!scales(a[8], c.out_dtype, size[0], size[1] * size[2], &c.scale, &c.scale_stride)) return false;
+        c.tokens = size[0];
+        c.heads = (int32_t)size[1];
+        c.d = (int32_t)size[2];
+        enqueue(status, a[0], c);
+        return true;
+    });
+}
+
+// quantize_weight(fn, weight, out, scale)
+PyObject *quantize_weight(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 4) Py_RETURN_NONE;
+    return guarded([&](int32_t &status) {
+        lq_weight c = {};
+        const at::Tensor *w, *t;
+        const void *p;
+        void *v;
+        if (!device(a[1], false, &w, &v) || w->dim() != 2 || !here(a, 1, 4)) return false;
+        const int64_t size[2] = {w->size(0), w->size(1)}, scale[2] = {blocks(size[0]), blocks(size[1])};
+        if (size[0] > INT32_MAX || size[1] > INT32_MAX) return false;
+        if (!token_rows(a[1], 2, size, &c.w, &c.w_stride, &w) || !token_type(*w, &c.dtype)) return false;
+        if (!token_rows(a[2], 2, size, &p, &c.out_stride, &t) || t->scalar_type() != E4M3) return false;
+        c.out = (void *)p;
+        if (!dense(a[3], 2, scale, F, false, &v)) return false;
+        c.scale = (float *)v;
+        c.n = (int32_t)size[0];
+        c.k = (int32_t)size[1];
+        enqueue(status, a[0], c);
+        return true;
+    });
+}
+
+// matmul(fn, workspace_bytes fn, x, x_scale, weight, weight_scale, out, bias, workspace or None)
+PyObject *matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 9) Py_RETURN_NONE;
+    return guarded([&](int32_t &status) {
+        lq_matmul c = {};
+        const at::Tensor *x, *w, *t;
+        const void *p;
+        void *v;
+        if (!device(a[2], false, &x, &v) || x->dim() != 2 || !device(a[4], false, &w, &v) || w->dim() != 2 || !here(a, 2, 9))
+            return false;
+        const int64_t T = x->size(0), k = x->size(1), m = w->size(0);
+        if (k > INT32_MAX || m > INT32_MAX) return false;
+        const int64_t xs[2] = {T, k}, ss[2] = {T, blocks(k)}, ws[2] = {m, k}, wss[2] = {blocks(m), blocks(k)}, os[2] = {T, m};
+        if (!token_rows(a[2], 2, xs, &c.x, &c.x_stride, &x) || x->scalar_type() != E4M3) return false;
+        if (!token_rows(a[3], 2, ss, &p, &c.x_scale_stride, &t) || t->scalar_type() != F) return false;
+        c.x_scale = (const float *)p;
+        if (!token_rows(a[4], 2, ws, &c.w, &c.w_stride, &w) || w->scalar_type() != E4M3) return false;
+        if (!dense(a[5], 2, wss, F, false, &v)) return false;
+        c.w_scale = (const float *)v;
+        if (!token_rows(a[6], 2, os, &p, &c.out_stride, &t) || !token_type(*t, &c.out_dtype)) return false;
+        c.out = (void *)p;
+        if (!vec(a[7], m, F, true, &c.bias)) return false;
+        c.tokens = T;
+        c.n = (int32_t)m;
+        c.k = (int32_t)k;
+        size_t need = 0;
+        using Size = int32_t (*)(const lq_matmul *, size_t *);
+        if (((Size)PyLong_AsVoidPtr(a[1]))(&c, &need) != LQ_OK) return false;
+        at::Tensor own;                 // freed into the allocator's pool of this stream after the launch
+        if (need) {
+            if (a[8] == Py_None) {
+                own = at::empty({(int64_t)need}, x->options().dtype(at::ScalarType::Byte));
+                c.workspace = own.data_ptr();
+            } else if (!tensor_ptr(a[8], need, (int)at::ScalarType::Byte, &c.workspace)) {
+                return false;
+            }
+            c.workspace_bytes = need;
+        }
+        enqueue(status, a[0], c);
+        return true;
+    });
+}
+
 // setup(lq_dims type, State type, field names, address of leapquant_state_bytes)
 PyObject *setup(PyObject *, PyObject *args) {
     PyObject *dims, *state, *names, *fn;
@@ -451,6 +633,10 @@ PyMethodDef methods[] = {
     {"conv", (PyCFunction)(void (*)(void))conv, METH_FASTCALL, "convolution, prompt or step"},
     {"qk_norm", (PyCFunction)(void (*)(void))qk_norm, METH_FASTCALL, "query and key norm"},
     {"scan", (PyCFunction)(void (*)(void))scan, METH_FASTCALL, "selective scan, prompt or step"},
+    {"add_norm", (PyCFunction)(void (*)(void))add_norm, METH_FASTCALL, "residual and norm"},
+    {"gate_norm", (PyCFunction)(void (*)(void))gate_norm, METH_FASTCALL, "gated norm"},
+    {"quantize_weight", (PyCFunction)(void (*)(void))quantize_weight, METH_FASTCALL, "a weight in E4M3"},
+    {"matmul", (PyCFunction)(void (*)(void))matmul, METH_FASTCALL, "product of E4M3 rows and a weight"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
