@@ -186,6 +186,161 @@ hipError_t launch_few(const ProductArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
+// ---- many tokens ------------------------------------------------------------------
+//
+// Bound: the matrix cores, with the LDS beside them.  A workgroup owns a tile of 16 WT TJ tokens x 16 WC TI channels, a wave
+// TJ x TI tiles of 16 x 16, all sums in registers.  Blocks of k are copied straight into LDS, STAGES - 1 ahead; a row's 8
+// pieces are placed by an exclusive or with bits of the row, so that the 16 rows that a read takes at once lie in 16 different
+// places of a 256-byte line of banks.  Channels are dealt to a wave's tiles so that a lane ends up with 4 TI
+// neighbouring ones of a token.
+__device__ const uint4 no_codes = {0, 0, 0, 0};
+
+// 16 bytes per lane into LDS, from a uniform base and a lane's offset (as dma16 otherwise)
+__device__ __forceinline__ void dma16_at(uint64_t base, uint32_t offset, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset), "s"(base), "s"(lds_base) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+
+template <int WT, int WC, int TJ, int TI, int STAGES>
+struct Tile {
+    static constexpr int WAVES = WT * WC, TOKENS = 16 * WT * TJ, CHANNELS = 16 * WC * TI;
+    static constexpr int X_COPIES = TOKENS / 8 / WAVES, W_COPIES = CHANNELS / 8 / WAVES;   // of 8 rows, per wave
+    static constexpr int COPIES = X_COPIES + W_COPIES + 1;                                 // ... and one of scales
+    static constexpr int STAGE = (TOKENS + CHANNELS) * BLOCK;
+    static_assert(TOKENS % (8 * WAVES) == 0 && CHANNELS % (8 * WAVES) == 0 && TOKENS % 64 == 0, "whole copies");
+};
+
+template <bool EXACT, int WT, int WC, int TJ, int TI, int STAGES>
+__global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, int tiles_t, int tiles_c) {
+    using T = Tile<WT, WC, TJ, TI, STAGES>;
+    __shared__ __attribute__((aligned(1024))) char codes[STAGES][T::STAGE];     // rows of x, then of w
+    __shared__ float scales[STAGES][T::TOKENS];
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wt = wave / WC, wc = wave % WC;
+
+    // Workgroups go round the 8 XCDs: each gets neighbouring tiles, GROUP of tokens side by side, whose rows its L2 shares.
+    constexpr int GROUP = 4;
+    const int total = tiles_t * tiles_c, per = total / 8, more = total % 8, xcd = blockIdx.x % 8;
+    const int id = xcd * per + min(xcd, more) + blockIdx.x / 8;
+    const int band = id / (GROUP * tiles_c), first = band * GROUP, high = min(GROUP, tiles_t - first);
+    const int in_band = id - band * GROUP * tiles_c;
+    const int t0 = (first + in_band % high) * T::TOKENS, c0 = in_band / high * T::CHANNELS;
+
+    // this lane's rows and pieces in the copies
+    const int row8 = lane >> 3, slot = lane & 7;
+    uint32_t xo[T::X_COPIES], wo[T::W_COPIES];
+    int xp[T::X_COPIES], wp[T::W_COPIES];
+#pragma unroll
+    for (int i = 0; i < T::X_COPIES; ++i) {
+        const int row = 8 * (wave * T::X_COPIES + i) + row8;
+        xp[i] = 16 * (slot ^ (row >> 1 & 7));
+        xo[i] = (uint32_t)(min(row, a.tokens - 1 - t0) * a.x_stride) + xp[i];
+    }
+#pragma unroll
+    for (int i = 0; i < T::W_COPIES; ++i) {
+        const int row = 8 * (wave * T::W_COPIES + i) + row8;
+        wp[i] = 16 * (slot ^ ((row / (4 * TI) & 3) | (row >> 1 & 1) << 2));
+        wo[i] = (uint32_t)(min(row, a.n - 1 - c0) * a.w_stride) + wp[i];
+    }
+    const uint64_t xbase = (uint64_t)(a.x + t0 * a.x_stride), wbase = (uint64_t)(a.w + c0 * a.w_stride);
+    const int scale_part = wave % (T::TOKENS / 64);
+    const float *scale_row = a.xs + min(t0 + 64 * scale_part + lane, a.tokens - 1) * a.xs_stride;
+    const int whole = a.k / BLOCK;
+
+    auto copy = [&](int b) {
+        const int st = b % STAGES;
+        const uint32_t xl = lds_addr(codes[st]) + wave * T::X_COPIES * 1024;
+        const uint32_t wl = lds_addr(codes[st]) + T::TOKENS * BLOCK + wave * T::W_COPIES * 1024;
+        const uint64_t at = (uint64_t)b * BLOCK;
+        if (b < whole) {
+#pragma unroll
+            for (int i = 0; i < T::X_COPIES; ++i) dma16_at(xbase + at, xo[i], xl + 1024 * i);
+#pragma unroll
+            for (int i = 0; i < T::W_COPIES; ++i) dma16_at(wbase + at, wo[i], wl + 1024 * i);
+        } else {                                    // the last block where it is shorter: zeros past k
+            const int left = a.k - b * BLOCK;
+#pragma unroll
+            for (int i = 0; i < T::X_COPIES; ++i) dma16(xp[i] < left ? (const char *)(xbase + at + xo[i]) : (const char *)&no_codes, xl + 1024 * i);
+#pragma unroll
+            for (int i = 0; i < T::W_COPIES; ++i) dma16(wp[i] < left ? (const char *)(wbase + at + wo[i]) : (const char *)&no_codes, wl + 1024 * i);
+        }
+        dma_element<4>(scale_row + b, lds_addr(scales[st]) + 256 * scale_part);
+    };
+
+    f32x4 acc[TI][TJ] = {};
+    // lane addresses of its operand rows (pieces g; pieces g + 4 lie 64 bytes on or back)
+    const int xr = 16 * TJ * wt + l16, wr = 16 * TI * wc + 4 * TI * (l16 >> 2) + (l16 & 3);
+    const int xa = xr * BLOCK + 16 * (g ^ (l16 >> 1));
+    const int wa = T::TOKENS * BLOCK + wr * BLOCK + 16 * (g ^ ((l16 >> 2) | (l16 >> 1 & 1) << 2));
+    const float *ws_row = a.ws + (int64_t)(min(c0 + 16 * TI * wc, a.n - 1) / BLOCK) * a.blocks;
+    float ws_lane = 0.0f;                           // the weight's scales of 64 blocks, one a lane
+
+#pragma unroll
+    for (int b = 0; b < STAGES - 1; ++b)
+        if (b < a.blocks) copy(b);
+    for (int b = 0; b < a.blocks; ++b) {
+        if (a.blocks - 1 - b >= STAGES - 2) wait_vm<T::COPIES *(STAGES - 2)>();
+        else wait_vm_all();
+        __syncthreads();
+        if ((b & 63) == 0) {
+            ws_lane = ws_row[min(b + lane, a.blocks - 1)];
+            asm volatile("" : "+v"(ws_lane));       // (its wait belongs here, not into every step)
+        }
+        if (b + STAGES - 1 < a.blocks) copy(b + STAGES - 1);
+        const char *from = codes[b % STAGES];
+        const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws_lane), b & 63));
+        Operand<EXACT> w[TI], x[2];
+        f32x4 part[3];
+        float f[TJ];
+        auto read_w = [&](int i) {
+            // (tile i's rows lie 4 i further on: 4 i changes no bit that the placement reads)
+            const char *p = from + 4 * i * BLOCK;
+            w[i].set(*(const uint4 *)(p + wa), *(const uint4 *)(p + (wa ^ 64)));
+        };
+        auto read_x = [&](int j) {
+            const char *p = from + 16 * j * BLOCK;
+            x[j & 1].set(*(const uint4 *)(p + xa), *(const uint4 *)(p + (xa ^ 64)));
+            f[j] = scales[b % STAGES][16 * TJ * wt + 16 * j + l16];
+        };
+        read_w(0);
+        read_x(0);
+#pragma unroll
+        for (int i = 1; i < TI; ++i) read_w(i);
+        // a tile's sums are added while the products of the next two run
+#pragma unroll
+        for (int q = 0; q < TI * TJ + 2; ++q) {
+            const int j = q / TI, i = q % TI;
+            if (i == 0 && j + 1 < TJ) read_x(j + 1);
+            if (q < TI * TJ) part[q % 3] = block_product(w[i], x[j & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (q > 1) {
+                const int jw = (q - 2) / TI, iw = (q - 2) % TI;
+                if (iw == 0) f[jw] *= ws;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[iw][jw][r] = fmaf(part[(q - 2) % 3][r], f[jw], acc[iw][jw][r]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) {
+        const int t = t0 + 16 * (TJ * wt + j) + l16, c = c0 + 16 * TI * wc + 4 * TI * g;
+#pragma unroll
+        for (int i = 0; i < TI; ++i) store4(a, t, c + 4 * i, acc[i][j]);
+    }
+}
+
+template <bool EXACT, int WT, int WC, int TJ, int TI, int STAGES>
+hipError_t launch_tiles(const ProductArgs &a, hipStream_t st) {
+    using T = Tile<WT, WC, TJ, TI, STAGES>;
+    const int tiles_t = (a.tokens - 1) / T::TOKENS + 1, tiles_c = (a.n - 1) / T::CHANNELS + 1;
+    const dim3 grid((unsigned)(tiles_t * tiles_c)), block(64 * T::WAVES);
+    hipLaunchKernelGGL((product_kernel<EXACT, WT, WC, TJ, TI, STAGES>), grid, block, 0, st, a, tiles_t, tiles_c);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t matmul_workspace_bytes(const lq_matmul &) { return 0; }
@@ -209,6 +364,9 @@ hipError_t launch_matmul(const lq_matmul &m, hipStream_t st) {
     a.blocks = (m.k + BLOCK - 1) / BLOCK;
     a.out_bf16 = m.out_dtype == LQ_TOKEN_BF16;
     if (m.tokens <= 16) return launch_few<1, 1, 8, 4>(a, st);
+    const int64_t large = (int64_t)((a.tokens - 1) / 256 + 1) * ((a.n - 1) / 256 + 1);
+    if (large >= 200) return a.out_bf16 ? launch_tiles<false, 2, 4, 8, 4, 2>(a, st) : launch_tiles<true, 2, 4, 8, 2, 3>(a, st);
+    if (m.tokens > 64) return a.out_bf16 ? launch_tiles<false, 2, 2, 4, 4, 4>(a, st) : launch_tiles<true, 2, 2, 4, 4, 4>(a, st);
     return launch_few<4, 4, 4, 1>(a, st);
 }
 
