@@ -191,16 +191,27 @@ hipError_t launch_few(const ProductArgs &a, hipStream_t st) {
 // Bound: the matrix cores, with the LDS beside them.  A workgroup owns a tile of 16 WT TJ tokens x 16 WC TI channels, a wave
 // TJ x TI tiles of 16 x 16, all sums in registers.  Blocks of k are copied straight into LDS, STAGES - 1 ahead; a row's 8
 // pieces are placed by an exclusive or with bits of the row, so that the 16 rows that a read takes at once lie in 16 different
-// places of a 256-byte line of banks.  Channels are dealt to a wave's tiles so that a lane ends up with 4 TI
-// neighbouring ones of a token.
+// places of a 256-byte line of banks.  Channels are dealt to a wave's tiles so that a lane ends up with 16 bytes of
+// neighbouring outputs of a token at a time, and 4 lanes with 64.
 __device__ const uint4 no_codes = {0, 0, 0, 0};
 
-// 16 bytes per lane into LDS, from a uniform base and a lane's offset (as dma16 otherwise)
-__device__ __forceinline__ void dma16_at(uint64_t base, uint32_t offset, uint32_t lds_base) {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset), "s"(base), "s"(lds_base) : "memory");
+// Copies into LDS as dma16's and dma_element's: 16 bytes per lane from a uniform base and a lane's offset, and one element.
+// Nothing is copied where `left` is not positive: no lane is on then (all are where these are called).  By the mask and
+// not by a branch, so that the products around them stay one run of instructions.
+__device__ __forceinline__ void dma16_if(int left, uint64_t base, uint32_t offset, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_cmp_gt_i32 %3, 0\n\ts_cselect_b64 exec, -1, 0\n\t"
+                 "global_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" :: "v"(offset), "s"(base), "s"(lds_base), "s"(left) : "memory", "scc");
 }
+__device__ __forceinline__ void dma4_if(int left, const void *g, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_cmp_gt_i32 %2, 0\n\ts_cselect_b64 exec, -1, 0\n\t"
+                 "global_load_lds_dword %0, off\n\ts_mov_b64 exec, -1" :: "v"(g), "s"(lds_base), "s"(left) : "memory", "scc");
+}
+// Waits until at most N copies are under way, or none where `more` is negative.
 template <int N>
-__device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+__device__ __forceinline__ void wait_copies(int more) {
+    if (N == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else asm volatile("s_cmp_ge_i32 %1, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(0)\n1:\n\ts_waitcnt vmcnt(%0)" :: "n"(N), "s"(more) : "memory", "scc");
+}
 
 template <int WT, int WC, int TJ, int TI, int STAGES>
 struct Tile {
@@ -209,7 +220,15 @@ struct Tile {
     static constexpr int COPIES = X_COPIES + W_COPIES + 1;                                 // ... and one of scales
     static constexpr int STAGE = (TOKENS + CHANNELS) * BLOCK;
     static_assert(TOKENS % (8 * WAVES) == 0 && CHANNELS % (8 * WAVES) == 0 && TOKENS % 64 == 0, "whole copies");
+    static_assert(TJ % 2 == 0 && TI % 2 == 0, "columns take turns in two registers, tiles of bf16 outputs go in pairs");
 };
+
+// Row m of a wave's tile i among its 16 TI rows of w, and the bits that place a row's pieces: they differ for the 8 pairs of
+// rows of a tile.
+template <bool EXACT>
+__device__ __forceinline__ int tile_row(int i, int m) { return EXACT ? 16 * i + m : 32 * (i >> 1) + 8 * (m >> 2) + 4 * (i & 1) + (m & 3); }
+template <bool EXACT>
+__device__ __forceinline__ int row_place(int row) { return EXACT ? row >> 1 & 7 : (row >> 3 & 3) | (row >> 1 & 1) << 2; }
 
 template <bool EXACT, int WT, int WC, int TJ, int TI, int STAGES>
 __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, int tiles_t, int tiles_c) {
@@ -241,7 +260,7 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
 #pragma unroll
     for (int i = 0; i < T::W_COPIES; ++i) {
         const int row = 8 * (wave * T::W_COPIES + i) + row8;
-        wp[i] = 16 * (slot ^ ((row / (4 * TI) & 3) | (row >> 1 & 1) << 2));
+        wp[i] = 16 * (slot ^ row_place<EXACT>(row));
         wo[i] = (uint32_t)(min(row, a.n - 1 - c0) * a.w_stride) + wp[i];
     }
     const uint64_t xbase = (uint64_t)(a.x + t0 * a.x_stride), wbase = (uint64_t)(a.w + c0 * a.w_stride);
@@ -249,86 +268,137 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
     const float *scale_row = a.xs + min(t0 + 64 * scale_part + lane, a.tokens - 1) * a.xs_stride;
     const int whole = a.k / BLOCK;
 
+    // whole block b on its way (not if there is none)
     auto copy = [&](int b) {
         const int st = b % STAGES;
         const uint32_t xl = lds_addr(codes[st]) + wave * T::X_COPIES * 1024;
         const uint32_t wl = lds_addr(codes[st]) + T::TOKENS * BLOCK + wave * T::W_COPIES * 1024;
         const uint64_t at = (uint64_t)b * BLOCK;
-        if (b < whole) {
+        const int left = whole - b;
 #pragma unroll
-            for (int i = 0; i < T::X_COPIES; ++i) dma16_at(xbase + at, xo[i], xl + 1024 * i);
+        for (int i = 0; i < T::X_COPIES; ++i) dma16_if(left, xbase + at, xo[i], xl + 1024 * i);
 #pragma unroll
-            for (int i = 0; i < T::W_COPIES; ++i) dma16_at(wbase + at, wo[i], wl + 1024 * i);
-        } else {                                    // the last block where it is shorter: zeros past k
-            const int left = a.k - b * BLOCK;
-#pragma unroll
-            for (int i = 0; i < T::X_COPIES; ++i) dma16(xp[i] < left ? (const char *)(xbase + at + xo[i]) : (const char *)&no_codes, xl + 1024 * i);
-#pragma unroll
-            for (int i = 0; i < T::W_COPIES; ++i) dma16(wp[i] < left ? (const char *)(wbase + at + wo[i]) : (const char *)&no_codes, wl + 1024 * i);
-        }
-        dma_element<4>(scale_row + b, lds_addr(scales[st]) + 256 * scale_part);
+        for (int i = 0; i < T::W_COPIES; ++i) dma16_if(left, wbase + at, wo[i], wl + 1024 * i);
+        dma4_if(left, scale_row + b, lds_addr(scales[st]) + 256 * scale_part);
     };
 
     f32x4 acc[TI][TJ] = {};
     // lane addresses of its operand rows (pieces g; pieces g + 4 lie 64 bytes on or back)
-    const int xr = 16 * TJ * wt + l16, wr = 16 * TI * wc + 4 * TI * (l16 >> 2) + (l16 & 3);
+    const int xr = 16 * TJ * wt + l16, wr = 16 * TI * wc + tile_row<EXACT>(0, l16);
     const int xa = xr * BLOCK + 16 * (g ^ (l16 >> 1));
-    const int wa = T::TOKENS * BLOCK + wr * BLOCK + 16 * (g ^ ((l16 >> 2) | (l16 >> 1 & 1) << 2));
+    const int wa = T::TOKENS * BLOCK + wr * BLOCK + 16 * (g ^ row_place<EXACT>(wr));
     const float *ws_row = a.ws + (int64_t)(min(c0 + 16 * TI * wc, a.n - 1) / BLOCK) * a.blocks;
     float ws_lane = 0.0f;                           // the weight's scales of 64 blocks, one a lane
 
-#pragma unroll
-    for (int b = 0; b < STAGES - 1; ++b)
-        if (b < a.blocks) copy(b);
-    for (int b = 0; b < a.blocks; ++b) {
-        if (a.blocks - 1 - b >= STAGES - 2) wait_vm<T::COPIES *(STAGES - 2)>();
-        else wait_vm_all();
+    // Operands are read from LDS ahead of their use: a column's x while the column before is multiplied, the next block's
+    // first ones while this block's last column is.  So all of a block has been read, and its place is free, before
+    // its last column, which is where the waves meet and the next copies are sent.
+    Operand<EXACT> w[TI], x[2];
+    float f[2];
+    auto read_w = [&](int b, int i) {
+        // (where tile i's rows lie, further on by its first one, changes no bit that the placement reads)
+        const char *p = codes[b % STAGES] + tile_row<EXACT>(i, 0) * BLOCK;
+        w[i].set(*(const uint4 *)(p + wa), *(const uint4 *)(p + (wa ^ 64)));
+    };
+    auto read_x = [&](int b, int j) {
+        const char *p = codes[b % STAGES] + 16 * j * BLOCK;
+        x[j & 1].set(*(const uint4 *)(p + xa), *(const uint4 *)(p + (xa ^ 64)));
+        f[j & 1] = scales[b % STAGES][16 * TJ * wt + 16 * j + l16];
+    };
+    // (what was read before is in registers when the waves meet)
+    auto meet = [&](int b) {
+        wait_copies<T::COPIES *(STAGES - 2)>(whole + 1 - STAGES - b);
         __syncthreads();
+    };
+    auto multiply = [&](int b, bool ahead) {
         if ((b & 63) == 0) {
             ws_lane = ws_row[min(b + lane, a.blocks - 1)];
-            asm volatile("" : "+v"(ws_lane));       // (its wait belongs here, not into every step)
+            asm volatile("" : "+v"(ws_lane));       // (its wait belongs here, not into every block)
         }
-        if (b + STAGES - 1 < a.blocks) copy(b + STAGES - 1);
-        const char *from = codes[b % STAGES];
         const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws_lane), b & 63));
-        Operand<EXACT> w[TI], x[2];
         f32x4 part[3];
-        float f[TJ];
-        auto read_w = [&](int i) {
-            // (tile i's rows lie 4 i further on: 4 i changes no bit that the placement reads)
-            const char *p = from + 4 * i * BLOCK;
-            w[i].set(*(const uint4 *)(p + wa), *(const uint4 *)(p + (wa ^ 64)));
-        };
-        auto read_x = [&](int j) {
-            const char *p = from + 16 * j * BLOCK;
-            x[j & 1].set(*(const uint4 *)(p + xa), *(const uint4 *)(p + (xa ^ 64)));
-            f[j] = scales[b % STAGES][16 * TJ * wt + 16 * j + l16];
-        };
-        read_w(0);
-        read_x(0);
-#pragma unroll
-        for (int i = 1; i < TI; ++i) read_w(i);
+        float scale[2];
         // a tile's sums are added while the products of the next two run
 #pragma unroll
         for (int q = 0; q < TI * TJ + 2; ++q) {
             const int j = q / TI, i = q % TI;
-            if (i == 0 && j + 1 < TJ) read_x(j + 1);
+            if (q < TI * TJ && i == 0) {
+                scale[j & 1] = f[j & 1] * ws;
+                if (j + 1 < TJ) {
+                    read_x(b, j + 1);
+                } else if (ahead) {
+                    meet(b + 1);
+                    copy(b + STAGES);
+                    read_x(b + 1, 0);
+                }
+            }
             if (q < TI * TJ) part[q % 3] = block_product(w[i], x[j & 1]);
             __builtin_amdgcn_sched_barrier(0);
+            if (ahead && q < TI * TJ && j == TJ - 1) read_w(b + 1, i);
             if (q > 1) {
                 const int jw = (q - 2) / TI, iw = (q - 2) % TI;
-                if (iw == 0) f[jw] *= ws;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[iw][jw][r] = fmaf(part[(q - 2) % 3][r], f[jw], acc[iw][jw][r]);
+                for (int r = 0; r < 4; ++r) acc[iw][jw][r] = fmaf(part[(q - 2) % 3][r], scale[jw & 1], acc[iw][jw][r]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    auto begin = [&](int b) {
+        read_x(b, 0);
+#pragma unroll
+        for (int i = 0; i < TI; ++i) read_w(b, i);
+    };
+    if (whole > 0) {
+#pragma unroll
+        for (int b = 0; b < STAGES - 1; ++b) copy(b);
+        meet(0);
+        copy(STAGES - 1);
+        begin(0);
+        // (after the last one it reads what lies there, for nobody)
+        for (int b = 0; b < whole; ++b) multiply(b, true);
     }
+    if (whole < a.blocks) {                         // a last block that is shorter: zeros past k
+        const int left = a.k - whole * BLOCK, st = whole % STAGES;
+        const uint32_t xl = lds_addr(codes[st]) + wave * T::X_COPIES * 1024;
+        const uint32_t wl = lds_addr(codes[st]) + T::TOKENS * BLOCK + wave * T::W_COPIES * 1024;
+        const char *none = (const char *)&no_codes, *x0 = (const char *)xbase + whole * BLOCK, *w0 = (const char *)wbase + whole * BLOCK;
+        __syncthreads();
 #pragma unroll
-    for (int j = 0; j < TJ; ++j) {
-        const int t = t0 + 16 * (TJ * wt + j) + l16, c = c0 + 16 * TI * wc + 4 * TI * g;
+        for (int i = 0; i < T::X_COPIES; ++i) dma16(xp[i] < left ? x0 + xo[i] : none, xl + 1024 * i);
 #pragma unroll
-        for (int i = 0; i < TI; ++i) store4(a, t, c + 4 * i, acc[i][j]);
+        for (int i = 0; i < T::W_COPIES; ++i) dma16(wp[i] < left ? w0 + wo[i] : none, wl + 1024 * i);
+        dma_element<4>(scale_row + whole, lds_addr(scales[st]) + 256 * scale_part);
+        wait_vm_all();
+        __syncthreads();
+        begin(whole);
+        multiply(whole, false);
+    }
+    // A lane has runs of 8 (bf16) or 4 (fp32) neighbouring channels of TJ tokens.
+    const int c = c0 + 16 * TI * wc;
+    if (c0 + T::CHANNELS <= a.n) {
+        float bias[TI][4];
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) bias[i][r] = a.bias ? a.bias[c + tile_row<EXACT>(i, 4 * g) + r] : 0.0f;
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+            const int t = t0 + 16 * (TJ * wt + j) + l16;
+            char *at = a.out + t * a.out_stride + (int64_t)c * (EXACT ? 4 : 2);
+            if (t >= a.tokens) continue;
+#pragma unroll
+            for (int i = 0; i < TI; i += EXACT ? 1 : 2) {
+                float v[8];
+#pragma unroll
+                for (int r = 0; r < (EXACT ? 4 : 8); ++r) v[r] = acc[i + r / 4][j][r % 4] + bias[i + r / 4][r % 4];
+                store_tok<!EXACT, EXACT ? 4 : 8>(at + tile_row<EXACT>(i, 4 * g) * (EXACT ? 4 : 2), v);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+#pragma unroll
+            for (int i = 0; i < TI; ++i) store4(a, t0 + 16 * (TJ * wt + j) + l16, c + tile_row<EXACT>(i, 4 * g), acc[i][j]);
     }
 }
 
