@@ -206,11 +206,11 @@ __device__ __forceinline__ void dma4_if(int left, const void *g, uint32_t lds_ba
     asm volatile("s_mov_b32 m0, %1\n\ts_cmp_gt_i32 %2, 0\n\ts_cselect_b64 exec, -1, 0\n\t"
                  "global_load_lds_dword %0, off\n\ts_mov_b64 exec, -1" :: "v"(g), "s"(lds_base), "s"(left) : "memory", "scc");
 }
-// Waits until at most N copies are under way, or none where `more` is negative.
-template <int N>
-__device__ __forceinline__ void wait_copies(int more) {
-    if (N == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    else asm volatile("s_cmp_ge_i32 %1, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(0)\n1:\n\ts_waitcnt vmcnt(%0)" :: "n"(N), "s"(more) : "memory", "scc");
+// Waits until at most `few` (which 1) or `many` (which 2) copies and stores are under way, or none (which 0).
+template <int FEW, int MANY>
+__device__ __forceinline__ void wait_copies(int which) {
+    asm volatile("s_cmp_gt_i32 %2, 1\n\ts_cbranch_scc1 2f\n\ts_cmp_gt_i32 %2, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(0)\n"
+                 "1:\n\ts_waitcnt vmcnt(%0)\n2:\n\ts_waitcnt vmcnt(%1)" :: "n"(FEW), "n"(MANY), "s"(which) : "memory", "scc");
 }
 
 template <int WT, int WC, int TJ, int TI, int STAGES>
@@ -219,7 +219,9 @@ struct Tile {
     static constexpr int X_COPIES = TOKENS / 8 / WAVES, W_COPIES = CHANNELS / 8 / WAVES;   // of 8 rows, per wave
     static constexpr int COPIES = X_COPIES + W_COPIES + 1;                                 // ... and one of scales
     static constexpr int STAGE = (TOKENS + CHANNELS) * BLOCK;
+    static constexpr int SCALES = TOKENS + 64;      // of the tokens, then of the weight's blocks beside them
     static_assert(TOKENS % (8 * WAVES) == 0 && CHANNELS % (8 * WAVES) == 0 && TOKENS % 64 == 0, "whole copies");
+    static_assert(TOKENS / 64 < WAVES, "a wave is left for the weight's scales");
     static_assert(TJ % 2 == 0 && TI % 2 == 0, "columns take turns in two registers, tiles of bf16 outputs go in pairs");
 };
 
@@ -234,107 +236,117 @@ template <bool EXACT, int WT, int WC, int TJ, int TI, int STAGES>
 __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, int tiles_t, int tiles_c) {
     using T = Tile<WT, WC, TJ, TI, STAGES>;
     __shared__ __attribute__((aligned(1024))) char codes[STAGES][T::STAGE];     // rows of x, then of w
-    __shared__ float scales[STAGES][T::TOKENS];
+    __shared__ float scales[STAGES][T::SCALES];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wt = wave / WC, wc = wave % WC;
+    const int whole = a.k / BLOCK, total = tiles_t * tiles_c;
 
     // Workgroups go round the 8 XCDs: each gets neighbouring tiles, GROUP of tokens side by side, whose rows its L2 shares.
-    constexpr int GROUP = 4;
-    const int total = tiles_t * tiles_c, per = total / 8, more = total % 8, xcd = blockIdx.x % 8;
-    const int id = xcd * per + min(xcd, more) + blockIdx.x / 8;
-    const int band = id / (GROUP * tiles_c), first = band * GROUP, high = min(GROUP, tiles_t - first);
-    const int in_band = id - band * GROUP * tiles_c;
-    const int t0 = (first + in_band % high) * T::TOKENS, c0 = in_band / high * T::CHANNELS;
-
-    // this lane's rows and pieces in the copies
-    const int row8 = lane >> 3, slot = lane & 7;
-    uint32_t xo[T::X_COPIES], wo[T::W_COPIES];
-    int xp[T::X_COPIES], wp[T::W_COPIES];
-#pragma unroll
-    for (int i = 0; i < T::X_COPIES; ++i) {
-        const int row = 8 * (wave * T::X_COPIES + i) + row8;
-        xp[i] = 16 * (slot ^ (row >> 1 & 7));
-        xo[i] = (uint32_t)(min(row, a.tokens - 1 - t0) * a.x_stride) + xp[i];
-    }
-#pragma unroll
-    for (int i = 0; i < T::W_COPIES; ++i) {
-        const int row = 8 * (wave * T::W_COPIES + i) + row8;
-        wp[i] = 16 * (slot ^ row_place<EXACT>(row));
-        wo[i] = (uint32_t)(min(row, a.n - 1 - c0) * a.w_stride) + wp[i];
-    }
-    const uint64_t xbase = (uint64_t)(a.x + t0 * a.x_stride), wbase = (uint64_t)(a.w + c0 * a.w_stride);
-    const int scale_part = wave % (T::TOKENS / 64);
-    const float *scale_row = a.xs + min(t0 + 64 * scale_part + lane, a.tokens - 1) * a.xs_stride;
-    const int whole = a.k / BLOCK;
-
-    // whole block b on its way (not if there is none)
-    auto copy = [&](int b) {
-        const int st = b % STAGES;
-        const uint32_t xl = lds_addr(codes[st]) + wave * T::X_COPIES * 1024;
-        const uint32_t wl = lds_addr(codes[st]) + T::TOKENS * BLOCK + wave * T::W_COPIES * 1024;
-        const uint64_t at = (uint64_t)b * BLOCK;
-        const int left = whole - b;
-#pragma unroll
-        for (int i = 0; i < T::X_COPIES; ++i) dma16_if(left, xbase + at, xo[i], xl + 1024 * i);
-#pragma unroll
-        for (int i = 0; i < T::W_COPIES; ++i) dma16_if(left, wbase + at, wo[i], wl + 1024 * i);
-        dma4_if(left, scale_row + b, lds_addr(scales[st]) + 256 * scale_part);
+    struct Place {
+        int t0, c0;
+    };
+    auto place = [&](int turn) {
+        constexpr int GROUP = 4;
+        const int xcd = turn % 8, id = xcd * (total / 8) + min(xcd, total % 8) + turn / 8;
+        const int band = id / (GROUP * tiles_c), first = band * GROUP, high = min(GROUP, tiles_t - first);
+        const int in_band = id - band * GROUP * tiles_c;
+        return Place{(first + in_band % high) * T::TOKENS, in_band / high * T::CHANNELS};
     };
 
-    f32x4 acc[TI][TJ] = {};
+    // ---- copies: the blocks of this workgroup's tiles, one after the other ----
+    const int row8 = lane >> 3, slot = lane & 7;
+    auto piece_x = [&](int i) { return 16 * (slot ^ (8 * (wave * T::X_COPIES + i) + row8 >> 1 & 7)); };
+    auto piece_w = [&](int i) { return 16 * (slot ^ row_place<EXACT>(8 * (wave * T::W_COPIES + i) + row8)); };
+    uint32_t xo[T::X_COPIES], wo[T::W_COPIES];      // this lane's rows and pieces
+    uint64_t xbase, wbase;
+    const float *scale_row;
+    int to_copy = 0, copied = 0, place_of_copy = 0; // blocks of the tile not sent yet, blocks sent in all, their place in LDS
+    int turn = blockIdx.x - gridDim.x;
+    auto next_tile = [&]() {                        // the copies go on with the next tile, if there is one
+        if (to_copy > 0 || turn + (int)gridDim.x >= total) return;
+        turn += gridDim.x;
+        const Place at = place(turn);
+#pragma unroll
+        for (int i = 0; i < T::X_COPIES; ++i)
+            xo[i] = (uint32_t)(min(8 * (wave * T::X_COPIES + i) + row8, a.tokens - 1 - at.t0) * a.x_stride) + piece_x(i);
+#pragma unroll
+        for (int i = 0; i < T::W_COPIES; ++i)
+            wo[i] = (uint32_t)(min(8 * (wave * T::W_COPIES + i) + row8, a.n - 1 - at.c0) * a.w_stride) + piece_w(i);
+        xbase = (uint64_t)(a.x + at.t0 * a.x_stride);
+        wbase = (uint64_t)(a.w + at.c0 * a.w_stride);
+        scale_row = wave < T::TOKENS / 64 ? a.xs + min(at.t0 + 64 * wave + lane, a.tokens - 1) * a.xs_stride
+                                          : a.ws + (int64_t)min(at.c0 / BLOCK + lane, (a.n - 1) / BLOCK) * a.blocks;
+        to_copy = whole;
+    };
+    const uint32_t xl = lds_addr(codes) + wave * T::X_COPIES * 1024, wl = lds_addr(codes) + T::TOKENS * BLOCK + wave * T::W_COPIES * 1024;
+    const uint32_t sl = lds_addr(scales) + 256 * min(wave, T::TOKENS / 64);
+    auto copy = [&]() {                             // the next block on its way (nothing if there is none)
+#pragma unroll
+        for (int i = 0; i < T::X_COPIES; ++i) dma16_if(to_copy, xbase, xo[i], xl + place_of_copy * T::STAGE + 1024 * i);
+#pragma unroll
+        for (int i = 0; i < T::W_COPIES; ++i) dma16_if(to_copy, wbase, wo[i], wl + place_of_copy * T::STAGE + 1024 * i);
+        dma4_if(to_copy, scale_row, sl + place_of_copy * (T::SCALES * 4));
+        xbase += BLOCK;
+        wbase += BLOCK;
+        ++scale_row;
+        copied += to_copy > 0;
+        --to_copy;
+        place_of_copy = place_of_copy + 1 == STAGES ? 0 : place_of_copy + 1;
+    };
+
+    // ---- products ----
+    f32x4 acc[TI][TJ];
     // lane addresses of its operand rows (pieces g; pieces g + 4 lie 64 bytes on or back)
     const int xr = 16 * TJ * wt + l16, wr = 16 * TI * wc + tile_row<EXACT>(0, l16);
     const int xa = xr * BLOCK + 16 * (g ^ (l16 >> 1));
     const int wa = T::TOKENS * BLOCK + wr * BLOCK + 16 * (g ^ row_place<EXACT>(wr));
-    const float *ws_row = a.ws + (int64_t)(min(c0 + 16 * TI * wc, a.n - 1) / BLOCK) * a.blocks;
-    float ws_lane = 0.0f;                           // the weight's scales of 64 blocks, one a lane
 
     // Operands are read from LDS ahead of their use: a column's x while the column before is multiplied, the next block's
     // first ones while this block's last column is.  So all of a block has been read, and its place is free, before
     // its last column, which is where the waves meet and the next copies are sent.
     Operand<EXACT> w[TI], x[2];
-    float f[2];
-    auto read_w = [&](int b, int i) {
+    float f[2], ws;
+    auto read_w = [&](int at, int i) {
         // (where tile i's rows lie, further on by its first one, changes no bit that the placement reads)
-        const char *p = codes[b % STAGES] + tile_row<EXACT>(i, 0) * BLOCK;
+        const char *p = codes[at] + tile_row<EXACT>(i, 0) * BLOCK;
         w[i].set(*(const uint4 *)(p + wa), *(const uint4 *)(p + (wa ^ 64)));
     };
-    auto read_x = [&](int b, int j) {
-        const char *p = codes[b % STAGES] + 16 * j * BLOCK;
+    auto read_x = [&](int at, int j) {
+        const char *p = codes[at] + 16 * j * BLOCK;
         x[j & 1].set(*(const uint4 *)(p + xa), *(const uint4 *)(p + (xa ^ 64)));
-        f[j & 1] = scales[b % STAGES][16 * TJ * wt + 16 * j + l16];
+        f[j & 1] = scales[at][16 * TJ * wt + 16 * j + l16];
+        if (j == 0) ws = scales[at][T::TOKENS + 16 * TI * wc / BLOCK];
     };
-    // (what was read before is in registers when the waves meet)
-    auto meet = [&](int b) {
-        wait_copies<T::COPIES *(STAGES - 2)>(whole + 1 - STAGES - b);
+    int used = 0, stored = 0;       // blocks that were waited for; of the waits to come, how many have a tile's stores before them
+    constexpr int STORES = TJ * TI / (EXACT ? 1 : 2), LATER = T::COPIES * (STAGES - 2);
+    // the next block is here (and what was read before is in registers)
+    auto meet = [&]() {
+        ++used;
+        wait_copies<LATER, LATER + STORES>(__builtin_amdgcn_readfirstlane(copied - used < STAGES - 2 ? 0 : stored > 0 ? 2 : 1));
+        --stored;
         __syncthreads();
     };
-    auto multiply = [&](int b, bool ahead) {
-        if ((b & 63) == 0) {
-            ws_lane = ws_row[min(b + lane, a.blocks - 1)];
-            asm volatile("" : "+v"(ws_lane));       // (its wait belongs here, not into every block)
-        }
-        const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws_lane), b & 63));
+    auto multiply = [&](int at, int next, bool ahead) {
         f32x4 part[3];
-        float scale[2];
+        float scale[2], wsb = ws;
         // a tile's sums are added while the products of the next two run
 #pragma unroll
         for (int q = 0; q < TI * TJ + 2; ++q) {
             const int j = q / TI, i = q % TI;
             if (q < TI * TJ && i == 0) {
-                scale[j & 1] = f[j & 1] * ws;
+                scale[j & 1] = f[j & 1] * wsb;
                 if (j + 1 < TJ) {
-                    read_x(b, j + 1);
+                    read_x(at, j + 1);
                 } else if (ahead) {
-                    meet(b + 1);
-                    copy(b + STAGES);
-                    read_x(b + 1, 0);
+                    meet();
+                    copy();
+                    read_x(next, 0);
                 }
             }
             if (q < TI * TJ) part[q % 3] = block_product(w[i], x[j & 1]);
             __builtin_amdgcn_sched_barrier(0);
-            if (ahead && q < TI * TJ && j == TJ - 1) read_w(b + 1, i);
+            if (ahead && q < TI * TJ && j == TJ - 1) read_w(next, i);
             if (q > 1) {
                 const int jw = (q - 2) / TI, iw = (q - 2) % TI;
 #pragma unroll
@@ -343,70 +355,102 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto begin = [&](int b) {
-        read_x(b, 0);
+    auto begin = [&](int at) {
+        read_x(at, 0);
 #pragma unroll
-        for (int i = 0; i < TI; ++i) read_w(b, i);
+        for (int i = 0; i < TI; ++i) read_w(at, i);
     };
-    if (whole > 0) {
-#pragma unroll
-        for (int b = 0; b < STAGES - 1; ++b) copy(b);
-        meet(0);
-        copy(STAGES - 1);
-        begin(0);
-        // (after the last one it reads what lies there, for nobody)
-        for (int b = 0; b < whole; ++b) multiply(b, true);
-    }
-    if (whole < a.blocks) {                         // a last block that is shorter: zeros past k
-        const int left = a.k - whole * BLOCK, st = whole % STAGES;
-        const uint32_t xl = lds_addr(codes[st]) + wave * T::X_COPIES * 1024;
-        const uint32_t wl = lds_addr(codes[st]) + T::TOKENS * BLOCK + wave * T::W_COPIES * 1024;
-        const char *none = (const char *)&no_codes, *x0 = (const char *)xbase + whole * BLOCK, *w0 = (const char *)wbase + whole * BLOCK;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < T::X_COPIES; ++i) dma16(xp[i] < left ? x0 + xo[i] : none, xl + 1024 * i);
-#pragma unroll
-        for (int i = 0; i < T::W_COPIES; ++i) dma16(wp[i] < left ? w0 + wo[i] : none, wl + 1024 * i);
-        dma_element<4>(scale_row + whole, lds_addr(scales[st]) + 256 * scale_part);
-        wait_vm_all();
-        __syncthreads();
-        begin(whole);
-        multiply(whole, false);
-    }
-    // A lane has runs of 8 (bf16) or 4 (fp32) neighbouring channels of TJ tokens.
-    const int c = c0 + 16 * TI * wc;
-    if (c0 + T::CHANNELS <= a.n) {
-        float bias[TI][4];
+    auto clear = [&]() {
 #pragma unroll
         for (int i = 0; i < TI; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) bias[i][r] = a.bias ? a.bias[c + tile_row<EXACT>(i, 4 * g) + r] : 0.0f;
+            for (int j = 0; j < TJ; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    };
+    // A lane has runs of 8 (bf16) or 4 (fp32) neighbouring channels of TJ tokens.
+    auto store = [&](const Place &tile) {
+        const int c = tile.c0 + 16 * TI * wc;
+        if (tile.c0 + T::CHANNELS <= a.n && tile.t0 + T::TOKENS <= a.tokens) {
+            float bias[TI][4];
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) {
-            const int t = t0 + 16 * (TJ * wt + j) + l16;
-            char *at = a.out + t * a.out_stride + (int64_t)c * (EXACT ? 4 : 2);
-            if (t >= a.tokens) continue;
+            for (int i = 0; i < TI; ++i)
 #pragma unroll
-            for (int i = 0; i < TI; i += EXACT ? 1 : 2) {
-                float v[8];
+                for (int r = 0; r < 4; ++r) bias[i][r] = a.bias ? a.bias[c + tile_row<EXACT>(i, 4 * g) + r] : 0.0f;
 #pragma unroll
-                for (int r = 0; r < (EXACT ? 4 : 8); ++r) v[r] = acc[i + r / 4][j][r % 4] + bias[i + r / 4][r % 4];
-                store_tok<!EXACT, EXACT ? 4 : 8>(at + tile_row<EXACT>(i, 4 * g) * (EXACT ? 4 : 2), v);
+            for (int j = 0; j < TJ; ++j) {
+                char *at = a.out + (tile.t0 + 16 * (TJ * wt + j) + l16) * a.out_stride + (int64_t)c * (EXACT ? 4 : 2);
+#pragma unroll
+                for (int i = 0; i < TI; i += EXACT ? 1 : 2) {
+                    float v[8];
+#pragma unroll
+                    for (int r = 0; r < (EXACT ? 4 : 8); ++r) v[r] = acc[i + r / 4][j][r % 4] + bias[i + r / 4][r % 4];
+                    store_tok<!EXACT, EXACT ? 4 : 8>(at + tile_row<EXACT>(i, 4 * g) * (EXACT ? 4 : 2), v);
+                }
             }
+            stored = STAGES - 1;    // these STORES come after the copies of so many blocks
+        } else {
+#pragma unroll
+            for (int j = 0; j < TJ; ++j)
+#pragma unroll
+                for (int i = 0; i < TI; ++i) store4(a, tile.t0 + 16 * (TJ * wt + j) + l16, c + tile_row<EXACT>(i, 4 * g), acc[i][j]);
+            stored = 0;             // (their number is not known)
         }
-    } else {
+    };
+
+    int here = 0;                   // place in LDS of the block at hand
+    if (whole > 0) {
+        next_tile();
 #pragma unroll
-        for (int j = 0; j < TJ; ++j)
+        for (int b = 0; b < STAGES - 1; ++b) {
+            copy();
+            next_tile();
+        }
+        meet();
+        copy();
+        begin(0);
+    }
+    for (int mine = blockIdx.x; mine < total; mine += gridDim.x) {
+        const Place tile = place(mine);
+        clear();
+        for (int b = 0; b < whole; ++b) {
+            next_tile();
+            const int next = here + 1 == STAGES ? 0 : here + 1;
+            multiply(here, next, true);     // (after the last block it reads what lies there, for nobody)
+            here = next;
+        }
+        if (whole < a.blocks) {             // a last block that is shorter: zeros past k (the grid has a workgroup a tile then)
+            Place at = tile;
+            asm volatile("" : "+s"(at.t0), "+s"(at.c0));    // (addresses are made here, not kept through the loop above)
+            const int left = a.k - whole * BLOCK;
+            __syncthreads();
 #pragma unroll
-            for (int i = 0; i < TI; ++i) store4(a, t0 + 16 * (TJ * wt + j) + l16, c + tile_row<EXACT>(i, 4 * g), acc[i][j]);
+            for (int i = 0; i < T::X_COPIES; ++i) {
+                const int64_t row = min(at.t0 + 8 * (wave * T::X_COPIES + i) + row8, a.tokens - 1);
+                const char *from = a.x + row * a.x_stride + whole * BLOCK + piece_x(i);
+                dma16(piece_x(i) < left ? from : (const char *)&no_codes, xl + 1024 * i);
+            }
+#pragma unroll
+            for (int i = 0; i < T::W_COPIES; ++i) {
+                const int64_t row = min(at.c0 + 8 * (wave * T::W_COPIES + i) + row8, a.n - 1);
+                const char *from = a.w + row * a.w_stride + whole * BLOCK + piece_w(i);
+                dma16(piece_w(i) < left ? from : (const char *)&no_codes, wl + 1024 * i);
+            }
+            dma_element<4>((wave < T::TOKENS / 64 ? a.xs + min(at.t0 + 64 * wave + lane, a.tokens - 1) * a.xs_stride
+                                                  : a.ws + (int64_t)min(at.c0 / BLOCK + lane, (a.n - 1) / BLOCK) * a.blocks) + whole, sl);
+            wait_vm_all();
+            __syncthreads();
+            begin(0);
+            multiply(0, 0, false);
+        }
+        store(tile);
     }
 }
 
+// Workgroups: one for each CU, which takes tiles in turn; one a tile where k ends inside a block.
 template <bool EXACT, int WT, int WC, int TJ, int TI, int STAGES>
 hipError_t launch_tiles(const ProductArgs &a, hipStream_t st) {
     using T = Tile<WT, WC, TJ, TI, STAGES>;
-    const int tiles_t = (a.tokens - 1) / T::TOKENS + 1, tiles_c = (a.n - 1) / T::CHANNELS + 1;
-    const dim3 grid((unsigned)(tiles_t * tiles_c)), block(64 * T::WAVES);
+    const int tiles_t = (a.tokens - 1) / T::TOKENS + 1, tiles_c = (a.n - 1) / T::CHANNELS + 1, total = tiles_t * tiles_c;
+    const dim3 grid((unsigned)(a.k % BLOCK ? total : std::min(total, 256))), block(64 * T::WAVES);
     hipLaunchKernelGGL((product_kernel<EXACT, WT, WC, TJ, TI, STAGES>), grid, block, 0, st, a, tiles_t, tiles_c);
     return hipGetLastError();
 }
