@@ -551,9 +551,9 @@ int32_t leapquant_quantize_weight(const lq_weight *w, void *stream);
  * the bits above 2^-13 of the largest: a sum is off by about 1.4e-5 of the sums' size
  * beside its rounding, at most 7 * 2^-13 of its terms where it cancels (take fp32
  * outputs where that matters; they run at about half the rate).  k is a multiple of
- * 16, n any; rows of x and w are at most 2^23 elements apart.  Large weights on few tokens are split over k and need
- * a workspace (leapquant_matmul_workspace_bytes, often 0); results do not depend
- * on where it lies, and the order of sums is the same in every call of the same sizes.
+ * 16 up to 2^23, n any up to 2^26, tokens * n at most 2^36; rows of x and w are at
+ * most 2^23 elements apart, rows of x_scale 2^20.  The order of sums is the same in every call
+ * of the same sizes.
  */
 typedef struct {
     int64_t tokens;
@@ -566,14 +566,8 @@ typedef struct {
     const float *w_scale;       /* [ceil(n / 128)][ceil(k / 128)], dense            */
     const float *bias;          /* [n] or NULL (0)                                  */
     void *out;                  /* [tokens][n]                                      */
-    void *workspace;            /* 16-byte aligned device memory, overwritten       */
-    size_t workspace_bytes;
 } lq_matmul;
 int32_t leapquant_matmul(const lq_matmul *m, void *stream);
-
-/* leapquant_matmul_workspace_bytes -- host only: workspace (may be 0) that
- * leapquant_matmul needs for these tokens, n, k and out_dtype. */
-int32_t leapquant_matmul_workspace_bytes(const lq_matmul *m, size_t *bytes_out);
 
 /* Static description of a status code. */
 const char *leapquant_strerror(int32_t status);

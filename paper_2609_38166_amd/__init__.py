@@ -13,7 +13,7 @@ from .binding import (  # noqa: F401
     leapquant_check_error,
     leapquant_conv_prompt, leapquant_conv_step, leapquant_qk_norm, leapquant_scan_prompt, leapquant_scan_step,
     leapquant_scan_gates, leapquant_scan_workspace_bytes, leapquant_check_error_word,
-    leapquant_add_norm, leapquant_gate_norm, leapquant_quantize_weight, leapquant_matmul, leapquant_matmul_workspace_bytes,
+    leapquant_add_norm, leapquant_gate_norm, leapquant_quantize_weight, leapquant_matmul,
 )
 
 __all__ = [
@@ -24,5 +24,4 @@ __all__ = [
     "leapquant_conv_prompt", "leapquant_conv_step", "leapquant_qk_norm", "leapquant_scan_prompt",
     "leapquant_scan_step", "leapquant_scan_gates", "leapquant_scan_workspace_bytes", "leapquant_check_error_word",
     "leapquant_add_norm", "leapquant_gate_norm", "leapquant_quantize_weight", "leapquant_matmul",
-    "leapquant_matmul_workspace_bytes",
 ]

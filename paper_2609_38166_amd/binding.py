@@ -40,8 +40,7 @@ EXPORTS = ("leapquant_state_bytes", "leapquant_quantize_state", "leapquant_decod
            "leapquant_check_error", "leapquant_strerror", "leapquant_last_hip_error",
            "leapquant_conv_prompt", "leapquant_conv_step", "leapquant_qk_norm", "leapquant_scan_workspace_bytes",
            "leapquant_scan_prompt", "leapquant_scan_step", "leapquant_scan_gates",
-           "leapquant_add_norm", "leapquant_gate_norm", "leapquant_quantize_weight", "leapquant_matmul",
-           "leapquant_matmul_workspace_bytes")
+           "leapquant_add_norm", "leapquant_gate_norm", "leapquant_quantize_weight", "leapquant_matmul")
 
 
 class LeapQuantError(RuntimeError):
@@ -91,7 +90,7 @@ lq_gated = _struct("lq_gated", (("l", "tokens"), ("i", "heads d act gate_first w
 lq_weight = _struct("lq_weight", (("i", "n k dtype"), ("l", "w_stride out_stride"), ("p", "w out scale")))
 lq_matmul = _struct("lq_matmul", (("l", "tokens"), ("i", "n k out_dtype"),
                                   ("l", "x_stride x_scale_stride w_stride out_stride"),
-                                  ("p", "x x_scale w w_scale bias out workspace"), ("z", "workspace_bytes")))
+                                  ("p", "x x_scale w w_scale bias out")))
 
 
 _L = None
@@ -101,7 +100,7 @@ _M = None
 _FN = {"leapquant_decode_step": 0, "leapquant_decode_step_general": 0, "leapquant_decode_step_commit": 0,
        "leapquant_window_commit": 0, "leapquant_conv_prompt": 0, "leapquant_conv_step": 0, "leapquant_qk_norm": 0,
        "leapquant_scan_prompt": 0, "leapquant_scan_step": 0, "leapquant_scan_workspace_bytes": 0, "leapquant_add_norm": 0,
-       "leapquant_gate_norm": 0, "leapquant_quantize_weight": 0, "leapquant_matmul": 0, "leapquant_matmul_workspace_bytes": 0}
+       "leapquant_gate_norm": 0, "leapquant_quantize_weight": 0, "leapquant_matmul": 0}
 
 
 class _NoMarshal:
@@ -161,7 +160,6 @@ def _lib():
         L.leapquant_gate_norm.argtypes = [vp, vp]
         L.leapquant_quantize_weight.argtypes = [vp, vp]
         L.leapquant_matmul.argtypes = [vp, vp]
-        L.leapquant_matmul_workspace_bytes.argtypes = [vp, vp]
         L.leapquant_strerror.argtypes = [i32]
         L.leapquant_strerror.restype = C.c_char_p
         L.leapquant_last_hip_error.argtypes = []
@@ -785,41 +783,21 @@ def leapquant_quantize_weight(weight, out, scale, stream=None):
     _check(_lib().leapquant_quantize_weight(C.byref(a), _stream(stream)), "leapquant_quantize_weight")
 
 
-def leapquant_matmul(x, x_scale, weight, weight_scale, out, bias=None, workspace=None, stream=None):
+def leapquant_matmul(x, x_scale, weight, weight_scale, out, bias=None, stream=None):
     """out [tokens, n] (fp32 or bf16) = x [tokens, k] times weight [n, k] transposed, plus bias [n]: x float8_e4m3fn with x_scale
-    [tokens, ceil(k / 128)], weight float8_e4m3fn with weight_scale [ceil(n / 128), ceil(k / 128)].  The workspace, where
-    one is needed, is allocated here unless a uint8 tensor is given; a stream of the caller's needs one."""
+    [tokens, ceil(k / 128)], weight float8_e4m3fn with weight_scale [ceil(n / 128), ceil(k / 128)]."""
     if stream is None and (_M or _lib()):
-        status = _M.matmul(_FN["leapquant_matmul"], _FN["leapquant_matmul_workspace_bytes"], x, x_scale, weight, weight_scale, out,
-                           bias, workspace)
+        status = _M.matmul(_FN["leapquant_matmul"], x, x_scale, weight, weight_scale, out, bias)
         if status is not None:
             return _check(status, "leapquant_matmul")
     if x.dim() != 2 or weight.dim() != 2:
         raise ValueError("x must be [tokens, k] and weight [n, k]")
-    _here(x, x_scale, weight, weight_scale, out, bias, workspace)
+    _here(x, x_scale, weight, weight_scale, out, bias)
     (tokens, k), n = x.shape, weight.shape[0]
     px, xs = _rows(x, "x", (tokens, k), E4M3)
     pxs, xss = _rows(x_scale, "x_scale", (tokens, _blocks(k)), torch.float32)
     pw, ws = _rows(weight, "weight", (n, k), E4M3)
     pws = _dense(weight_scale, "weight_scale", (_blocks(n), _blocks(k)))
     po, os_ = _rows(out, "out", (tokens, n))
-    a = lq_matmul(tokens, n, k, _token(out, "out"), xs, xss, ws, os_, px, pxs, pw, pws, _dense(bias, "bias", (n,), optional=True), po,
-                  None, 0)
-    need = C.c_size_t(0)
-    _check(_lib().leapquant_matmul_workspace_bytes(C.byref(a), C.byref(need)), "leapquant_matmul_workspace_bytes")
-    if need.value:
-        if workspace is None:
-            if stream is not None:
-                raise ValueError(f"a call on a stream of the caller's needs a workspace of {need.value} bytes")
-            workspace = torch.empty(need.value, dtype=torch.uint8, device=x.device)
-        a.workspace, a.workspace_bytes = _device(workspace, "workspace", torch.uint8), workspace.numel()
-        _need(workspace, need.value, "workspace")
+    a = lq_matmul(tokens, n, k, _token(out, "out"), xs, xss, ws, os_, px, pxs, pw, pws, _dense(bias, "bias", (n,), optional=True), po)
     _check(_lib().leapquant_matmul(C.byref(a), _stream(stream)), "leapquant_matmul")
-
-
-def leapquant_matmul_workspace_bytes(tokens, n, k, out_dtype=torch.bfloat16) -> int:
-    """Workspace that leapquant_matmul needs for these sizes."""
-    need = C.c_size_t(0)
-    a = lq_matmul(tokens=tokens, n=n, k=k, out_dtype=_TOKEN[out_dtype])
-    _check(_lib().leapquant_matmul_workspace_bytes(C.byref(a), C.byref(need)), "leapquant_matmul_workspace_bytes")
-    return need.value

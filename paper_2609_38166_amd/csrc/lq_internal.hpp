@@ -57,7 +57,6 @@ hipError_t launch_scan_gates(const lq_dims &d, const lq_scan &s, float *alpha, f
 hipError_t launch_add_norm(const lq_add &a, hipStream_t st);
 hipError_t launch_gate_norm(const lq_gated &g, hipStream_t st);
 hipError_t launch_quantize_weight(const lq_weight &w, hipStream_t st);
-size_t matmul_workspace_bytes(const lq_matmul &m);
 hipError_t launch_matmul(const lq_matmul &m, hipStream_t st);
 
 // Bytes between the rows of a token array; of one row's, nobody has to set a stride.

@@ -75,43 +75,24 @@ int32_t leapquant_quantize_weight(const lq_weight *w, void *stream) {
     return hip_status(launch_quantize_weight(*w, (hipStream_t)stream));
 }
 
-// what: 0 the workspace's size (shapes only), 1 the product
-static int32_t check_matmul(const lq_matmul *m, int what) {
+int32_t leapquant_matmul(const lq_matmul *m, void *stream) {
     if (!m || m->n <= 0 || m->k <= 0 || !token_type(m->out_dtype)) return LQ_EINVAL;
     int32_t e;
     if ((e = check_tokens(m->tokens)) != LQ_OK) return e;
     if (m->k % 16) return LQ_EUNSUPPORTED;
-    // (tiles of 16 x 16 at the least: their number, and the tokens' as a second dimension of a grid)
-    const int64_t tiles_n = ((int64_t)m->n + 15) / 16, tiles_t = (m->tokens + 15) / 16;
-    if (tiles_n * tiles_t > MAX_BLOCKS || tiles_t > 65535 * 4LL) return LQ_EUNSUPPORTED;
-    if (!what) return LQ_OK;
-    const int64_t T = m->tokens, apart = 1 << 23;
-    if (T > 1 && m->x_stride > apart) return LQ_EUNSUPPORTED;
+    // (workgroups are counted in 32 bits with their work-items: 16 channels of few tokens, or at least 128 x 256 outputs)
+    if (m->n > 1 << 26 || m->tokens > (1LL << 36) / m->n) return LQ_EUNSUPPORTED;
+    // a tile's rows are addressed by 32 bits from its first one
+    const int64_t T = m->tokens, apart = 1 << 23, scales_apart = 1 << 20;
+    if (m->k > apart || (T > 1 && (m->x_stride > apart || m->x_scale_stride > scales_apart))) return LQ_EUNSUPPORTED;
     if (m->n > 1 && m->w_stride > apart) return LQ_EUNSUPPORTED;
+    if (((int64_t)m->n + 127) / 128 * (((int64_t)m->k + 127) / 128) > 1 << 29) return LQ_EUNSUPPORTED;
     if ((e = check_rows(m->x, T, m->k, m->x_stride, 1, 16)) != LQ_OK) return e;
     if ((e = check_scales(m->x_scale, T, m->k, m->x_scale_stride)) != LQ_OK) return e;
     if ((e = check_rows(m->w, m->n, m->k, m->w_stride, 1, 16)) != LQ_OK) return e;
     if ((e = check(m->w_scale, 4)) != LQ_OK) return e;
     if ((e = check(m->bias, 4, false)) != LQ_OK) return e;
-    return check_rows(m->out, T, m->n, m->out_stride, token_size(m->out_dtype), 16);
-}
-
-int32_t leapquant_matmul_workspace_bytes(const lq_matmul *m, size_t *bytes_out) {
-    const int32_t e = check_matmul(m, 0);
-    if (e != LQ_OK) return e;
-    if (!bytes_out) return LQ_EINVAL;
-    *bytes_out = matmul_workspace_bytes(*m);
-    return LQ_OK;
-}
-
-int32_t leapquant_matmul(const lq_matmul *m, void *stream) {
-    int32_t e = check_matmul(m, 1);
-    if (e != LQ_OK) return e;
-    const size_t need = matmul_workspace_bytes(*m);
-    if (need) {
-        if ((e = check(m->workspace, 16)) != LQ_OK) return e;
-        if (m->workspace_bytes < need) return LQ_EINVAL;
-    }
+    if ((e = check_rows(m->out, T, m->n, m->out_stride, token_size(m->out_dtype), 16)) != LQ_OK) return e;
     return hip_status(launch_matmul(*m, (hipStream_t)stream));
 }
 

@@ -558,44 +558,31 @@ PyObject *quantize_weight(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// matmul(fn, workspace_bytes fn, x, x_scale, weight, weight_scale, out, bias, workspace or None)
+// matmul(fn, x, x_scale, weight, weight_scale, out, bias)
 PyObject *matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    if (n != 9) Py_RETURN_NONE;
+    if (n != 7) Py_RETURN_NONE;
     return guarded([&](int32_t &status) {
         lq_matmul c = {};
         const at::Tensor *x, *w, *t;
         const void *p;
         void *v;
-        if (!device(a[2], false, &x, &v) || x->dim() != 2 || !device(a[4], false, &w, &v) || w->dim() != 2 || !here(a, 2, 9))
+        if (!device(a[1], false, &x, &v) || x->dim() != 2 || !device(a[3], false, &w, &v) || w->dim() != 2 || !here(a, 1, 7))
             return false;
         const int64_t T = x->size(0), k = x->size(1), m = w->size(0);
         if (k > INT32_MAX || m > INT32_MAX) return false;
         const int64_t xs[2] = {T, k}, ss[2] = {T, blocks(k)}, ws[2] = {m, k}, wss[2] = {blocks(m), blocks(k)}, os[2] = {T, m};
-        if (!token_rows(a[2], 2, xs, &c.x, &c.x_stride, &x) || x->scalar_type() != E4M3) return false;
-        if (!token_rows(a[3], 2, ss, &p, &c.x_scale_stride, &t) || t->scalar_type() != F) return false;
+        if (!token_rows(a[1], 2, xs, &c.x, &c.x_stride, &x) || x->scalar_type() != E4M3) return false;
+        if (!token_rows(a[2], 2, ss, &p, &c.x_scale_stride, &t) || t->scalar_type() != F) return false;
         c.x_scale = (const float *)p;
-        if (!token_rows(a[4], 2, ws, &c.w, &c.w_stride, &w) || w->scalar_type() != E4M3) return false;
-        if (!dense(a[5], 2, wss, F, false, &v)) return false;
+        if (!token_rows(a[3], 2, ws, &c.w, &c.w_stride, &w) || w->scalar_type() != E4M3) return false;
+        if (!dense(a[4], 2, wss, F, false, &v)) return false;
         c.w_scale = (const float *)v;
-        if (!token_rows(a[6], 2, os, &p, &c.out_stride, &t) || !token_type(*t, &c.out_dtype)) return false;
+        if (!token_rows(a[5], 2, os, &p, &c.out_stride, &t) || !token_type(*t, &c.out_dtype)) return false;
         c.out = (void *)p;
-        if (!vec(a[7], m, F, true, &c.bias)) return false;
+        if (!vec(a[6], m, F, true, &c.bias)) return false;
         c.tokens = T;
         c.n = (int32_t)m;
         c.k = (int32_t)k;
-        size_t need = 0;
-        using Size = int32_t (*)(const lq_matmul *, size_t *);
-        if (((Size)PyLong_AsVoidPtr(a[1]))(&c, &need) != LQ_OK) return false;
-        at::Tensor own;                 // freed into the allocator's pool of this stream after the launch
-        if (need) {
-            if (a[8] == Py_None) {
-                own = at::empty({(int64_t)need}, x->options().dtype(at::ScalarType::Byte));
-                c.workspace = own.data_ptr();
-            } else if (!tensor_ptr(a[8], need, (int)at::ScalarType::Byte, &c.workspace)) {
-                return false;
-            }
-            c.workspace_bytes = need;
-        }
         enqueue(status, a[0], c);
         return true;
     });

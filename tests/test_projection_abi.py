@@ -72,7 +72,9 @@ PRODUCT = [
     (dict(w_scale=GOOD + 2), EALIGN), (dict(bias=GOOD + 2), EALIGN), (dict(out=GOOD + 8), EALIGN), (dict(x_stride=240), EINVAL),
     (dict(x_stride=264), EALIGN), (dict(w_stride=255), EINVAL), (dict(w_stride=264), EALIGN), (dict(out_stride=199), EINVAL),
     (dict(out_stride=204), EALIGN), (dict(x_scale_stride=1), EINVAL), (dict(x_stride=(1 << 23) + 16), EUNSUP),
-    (dict(w_stride=(1 << 23) + 16), EUNSUP), (dict(tokens=(1 << 31) - 1, n=1 << 20), EUNSUP),
+    (dict(w_stride=(1 << 23) + 16), EUNSUP), (dict(x_scale_stride=(1 << 20) + 1), EUNSUP),
+    (dict(tokens=(1 << 31) - 1, n=1 << 20, out_stride=1 << 20), EUNSUP), (dict(n=(1 << 26) + 1, out_stride=1 << 27), EUNSUP),
+    (dict(n=1 << 26, k=1 << 22, w_stride=1 << 22, x_stride=1 << 22, out_stride=1 << 26, x_scale_stride=1 << 15), EUNSUP),
 ]
 
 
@@ -96,15 +98,10 @@ def test_matmul_refusals(kw, status):
     assert B.lib().leapquant_matmul(C.byref(product(**kw)), None) == status
 
 
-def test_null_structs_and_workspace_sizes():
+def test_null_structs():
     L = B.lib()
     assert L.leapquant_add_norm(None, None) == EINVAL and L.leapquant_gate_norm(None, None) == EINVAL
     assert L.leapquant_quantize_weight(None, None) == EINVAL and L.leapquant_matmul(None, None) == EINVAL
-    need = C.c_size_t(77)
-    assert L.leapquant_matmul_workspace_bytes(None, C.byref(need)) == EINVAL
-    assert L.leapquant_matmul_workspace_bytes(C.byref(product()), None) == EINVAL
-    assert L.leapquant_matmul_workspace_bytes(C.byref(product(k=24)), C.byref(need)) == EUNSUP and need.value == 77
-    assert L.leapquant_matmul_workspace_bytes(C.byref(B.lq_matmul(tokens=0, n=5, k=16)), C.byref(need)) == 0 and need.value == 0
 
 
 def test_no_tokens_need_no_arrays():
@@ -133,12 +130,6 @@ def test_the_binding_refuses_what_is_not_a_device_tensor_or_has_other_shapes():
         B.leapquant_quantize_weight(e(128), e(128, dtype=E4), e(1, 1))
     with pytest.raises(ValueError, match="x must be"):
         B.leapquant_matmul(e(128, dtype=E4), e(2, 1), e(4, 128, dtype=E4), e(1, 1), e(2, 4))
-
-
-def test_workspace_of_the_binding():
-    assert B.leapquant_matmul_workspace_bytes(0, 128, 128) == 0
-    with pytest.raises(B.LeapQuantError):
-        B.leapquant_matmul_workspace_bytes(4, 128, 100)
 
 
 G = dict(device="cuda")
@@ -203,7 +194,7 @@ def test_regular_calls_take_the_native_path_and_give_the_same():
             assert M.gate_norm(F["leapquant_gate_norm"], x.view(5, 2, 128), gate, g8, w[:128].contiguous(), 0, False, 1e-6, gs) == 0
             assert M.gate_norm(F["leapquant_gate_norm"], x.view(5, 2, 128), gate, g8, w.view(2, 128), 0, True, 1e-6, gs) == 0
             assert M.quantize_weight(F["leapquant_quantize_weight"], weight, w8, ws) == 0
-            assert M.matmul(F["leapquant_matmul"], F["leapquant_matmul_workspace_bytes"], o8, s, w8, ws, out, bias, None) == 0
+            assert M.matmul(F["leapquant_matmul"], o8, s, w8, ws, out, bias) == 0
         else:
             B.leapquant_add_norm(x, o8, residual=r, residual_out=ro, weight=w, scale=s, **kw)
             B.leapquant_gate_norm(x.view(5, 2, 128), gate, g8, weight=w[:128].contiguous(), scale=gs, **kw)
