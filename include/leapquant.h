@@ -508,8 +508,9 @@ int32_t leapquant_add_norm(const lq_add *a, void *stream);
  *   out = x / sqrt(mean x^2 + eps) * weight * a,  or, gate_first,
  *   out = x a / sqrt(mean (x a)^2 + eps) * weight.
  * d, the channels under one norm, is 64 or a multiple of 128 up to
- * LQ_MAX_NORM_CHANNELS.  The blocks of an E4M3 output run over the token's row of
- * heads * d channels.  out may be x or gate (same type and stride).
+ * LQ_MAX_NORM_CHANNELS; heads are at most 2^20.  The blocks of an E4M3 output run
+ * over the token's row of heads * d channels.  out may be x or gate (same type and
+ * stride).
  */
 typedef struct {
     int64_t tokens;

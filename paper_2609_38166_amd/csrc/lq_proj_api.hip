@@ -52,7 +52,7 @@ int32_t leapquant_gate_norm(const lq_gated *g, void *stream) {
     if (!flag(g->gate_first) || !flag(g->weight_heads) || !epsilon(g->eps)) return LQ_EINVAL;
     if ((e = check_tokens(g->tokens)) != LQ_OK) return e;
     if ((g->d != 64 && g->d % 128) || g->d > LQ_MAX_NORM_CHANNELS) return LQ_EUNSUPPORTED;
-    if (g->tokens * ((int64_t)g->heads + (g->d == 64 ? g->heads & 1 : 0)) > INT32_MAX) return LQ_EUNSUPPORTED;
+    if (g->heads > 1 << 20) return LQ_EUNSUPPORTED;      // (a workgroup each, at the most)
     const int64_t T = g->tokens, c = (int64_t)g->heads * g->d;
     if ((e = check_rows(g->x, T, c, g->x_stride, token_size(g->dtype), 16)) != LQ_OK) return e;
     if ((e = check_rows(g->gate, T, c, g->gate_stride, token_size(g->gate_dtype), 16)) != LQ_OK) return e;

@@ -21,7 +21,8 @@ struct RowArgs {
     float *scale;
     int64_t x_stride, second_stride, sum_stride, out_stride;    // bytes
     int64_t scale_stride;           // floats
-    uint32_t rows, heads, heads_turn;       // rows: tokens * heads_turn
+    uint32_t tokens, heads, heads_turn;     // rows: heads_turn a token, those past heads are none
+    uint32_t step;                  // a group of lanes takes every step-th token
     int32_t length, norm, out_type, act, first, weight_heads;
     float eps;
 };
@@ -60,68 +61,98 @@ __device__ __forceinline__ float row_sum(float x, float *sums) {
     return x;
 }
 
+// sigmoid(z) = 1 / (1 + e), or e / (1 + e) for z < 0, of e = exp(-|z|): the hardware's exponential of the rounded product with
+// log2(e), times 1 + what the rounding left (so a large |z| keeps its bits), and the hardware's reciprocal, 1 ulp each.  The
+// kernel is bound by such instructions: with expf and an IEEE division 8192 x 32 heads of 128 took 52 us.  (NaN gives
+// any number: see gate_values.)
+__device__ __forceinline__ float sigmoid(float z) {
+    const float a = fminf(fabsf(z), 150.0f);
+    const float t = -1.44269502f * a, rest = fmaf(a, -1.92596303e-8f, fmaf(a, -1.44269502f, -t));
+    const float e0 = __builtin_amdgcn_exp2f(t), e = fmaf(e0 * rest, 0.693147181f, e0);
+    const float r = __builtin_amdgcn_rcpf(1.0f + e);
+    return z < 0.0f ? e * r : r;
+}
+__device__ __forceinline__ void gate_values(float *z, int act) {
+    if (act == LQ_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] *= sigmoid(z[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = z[i] != z[i] ? z[i] : sigmoid(z[i]);
+    }
+}
+
+// A group of L lanes keeps its head (heads of the next tokens follow a constant distance on) and takes tokens in turn.
 template <int L, int P, bool XB, bool SB, bool GATE>
 __global__ __launch_bounds__(L > 256 ? L : 256) void rows_kernel(RowArgs a) {
     constexpr int THREADS = L > 256 ? L : 256, PER = THREADS / L;
     __shared__ float sums[L > 64 ? L / 64 : 1];
     const int l = threadIdx.x % L, l16 = threadIdx.x & 15;
+    const uint32_t row = blockIdx.x * PER + threadIdx.x / L;
+    uint32_t t = GATE ? row / a.heads_turn : row;
+    const uint32_t h = GATE ? row - t * a.heads_turn : 0;
+    const int64_t col = GATE ? (int64_t)h * a.length : 0;
+    const bool there = !GATE || h < a.heads;        // (the lanes of a head that is none take part in the exchanges)
+    if (t >= a.step) return;                        // (groups past step * heads_turn: whole pairs of heads)
     float w[P][8];
-    auto weights = [&](const float *from) {
+    bool in[P];
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const int c = 8 * (p * L + l);
+    for (int p = 0; p < P; ++p) {
+        const int c = 8 * (p * L + l);
+        in[p] = there && c < a.length;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[p][i] = 1.0f;
-            if (a.weight && c < a.length) {
-                const float4 u = *(const float4 *)(from + c), v = *(const float4 *)(from + c + 4);
-                w[p][0] = u.x; w[p][1] = u.y; w[p][2] = u.z; w[p][3] = u.w;
-                w[p][4] = v.x; w[p][5] = v.y; w[p][6] = v.z; w[p][7] = v.w;
-            }
+        for (int i = 0; i < 8; ++i) w[p][i] = 1.0f;
+        if (a.weight && in[p]) {
+            const float4 *from = (const float4 *)(a.weight + (a.weight_heads ? col : 0) + c);
+            const float4 u = from[0], v = from[1];
+            w[p][0] = u.x; w[p][1] = u.y; w[p][2] = u.z; w[p][3] = u.w;
+            w[p][4] = v.x; w[p][5] = v.y; w[p][6] = v.z; w[p][7] = v.w;
         }
-    };
-    if (!GATE || !a.weight_heads) weights(a.weight);
-    for (uint32_t r0 = blockIdx.x * PER; r0 < a.rows; r0 += gridDim.x * PER) {
-        const uint32_t row = r0 + threadIdx.x / L;
-        const uint32_t t = GATE ? row / a.heads_turn : row, h = GATE ? row - t * a.heads_turn : 0;
-        const bool here = row < a.rows && (!GATE || h < a.heads);       // (every lane takes part in the exchanges)
-        const int64_t col = GATE ? (int64_t)h * a.length : 0;
+    }
+    const char *x = a.x + t * a.x_stride + (col + 8 * l) * Tok<XB>::BYTES;
+    const char *second = a.second + t * a.second_stride + (col + 8 * l) * Tok<SB>::BYTES;
+    char *sum = GATE ? nullptr : a.sum + t * a.sum_stride + 8 * l * Tok<SB>::BYTES;
+    const int width = a.out_type == LQ_TOKEN_E4M3 ? 1 : a.out_type == LQ_TOKEN_BF16 ? 2 : 4;
+    char *out = a.out + t * a.out_stride + (col + 8 * l) * width;
+    float *scale = a.scale + t * a.scale_stride + (col + 8 * l) / BLOCK;
+    const bool with_second = GATE || a.second, with_sum = !GATE && a.sum;
+    for (; t < a.tokens; t += a.step) {
         Raw<XB> xr[P];
         Raw<SB> sr[P];
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const int c = 8 * (p * L + l);
-            if (here && c < a.length) {
-                xr[p].load(a.x + (int64_t)t * a.x_stride + (col + c) * Tok<XB>::BYTES);
-                if (GATE || a.second) sr[p].load(a.second + (int64_t)t * a.second_stride + (col + c) * Tok<SB>::BYTES);
+        for (int p = 0; p < P; ++p)
+            if (in[p]) {
+                xr[p].load(x + p * (8 * L * Tok<XB>::BYTES));
+                if (with_second) sr[p].load(second + p * (8 * L * Tok<SB>::BYTES));
             }
-        }
-        if (GATE && a.weight_heads && here) weights(a.weight + col);
         float y[P][8], ss = 0.0f;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const int c = 8 * (p * L + l);
-            if (here && c < a.length) {
-                float s[8];
-                xr[p].values(y[p]);
-                if (GATE || a.second) sr[p].values(s);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (GATE) {
-                        const float e = 1.0f + expf(-s[i]);
-                        const float g = (a.act == LQ_ACT_SILU ? s[i] : 1.0f) / e;
-                        if (a.first) y[p][i] *= g;
-                        else s[i] = g;
-                    } else if (a.second) {
-                        y[p][i] += s[i];
-                    }
-                    ss = fmaf(y[p][i], y[p][i], ss);
-                    if (GATE && !a.first) y[p][i] *= s[i];
-                }
-                if (!GATE && a.sum) store_tok<SB, 8>(a.sum + (int64_t)t * a.sum_stride + (int64_t)c * Tok<SB>::BYTES, y[p]);
-            } else {
+            if (!in[p]) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) y[p][i] = 0.0f;
+                continue;
             }
+            float s[8];
+            xr[p].values(y[p]);
+            if (with_second) sr[p].values(s);
+            if (GATE) {
+                gate_values(s, a.act);
+                if (a.first) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[p][i] *= s[i];
+                }
+            } else if (with_second) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[p][i] += s[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss = fmaf(y[p][i], y[p][i], ss);
+            if (GATE && !a.first) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[p][i] *= s[i];
+            }
+            if (with_sum) store_tok<SB, 8>(sum + p * (8 * L * Tok<SB>::BYTES), y[p]);
         }
         if (GATE || a.norm) {
             const float inv = 1.0f / sqrtf(row_sum<L>(ss, sums) / (float)a.length + a.eps);
@@ -130,33 +161,42 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rows_kernel(RowArgs a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) y[p][i] = y[p][i] * inv * w[p][i];
         }
+        if (a.out_type == LQ_TOKEN_E4M3) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const int c = 8 * (p * L + l);
-            const bool in = here && c < a.length;
-            if (a.out_type == LQ_TOKEN_E4M3) {
-                const float most = block_most(row16_most(in ? most8(y[p]) : 0u));
+            for (int p = 0; p < P; ++p) {
+                const float most = block_most(row16_most(in[p] ? most8(y[p]) : 0u));
                 const uint2 code = encode_e4m3(y[p], E4M3_MAX / most);
-                if (in) {
-                    *(uint2 *)(a.out + (int64_t)t * a.out_stride + col + c) = code;
-                    if (l16 == 0) a.scale[(int64_t)t * a.scale_stride + (col + c) / BLOCK] = most / E4M3_MAX;
+                if (in[p]) {
+                    *(uint2 *)(out + p * 8 * L) = code;
+                    if (l16 == 0) scale[p * 8 * L / BLOCK] = most / E4M3_MAX;
                 }
-            } else if (in) {
-                if (a.out_type == LQ_TOKEN_BF16) store_tok<true, 8>(a.out + (int64_t)t * a.out_stride + (col + c) * 2, y[p]);
-                else store_tok<false, 8>(a.out + (int64_t)t * a.out_stride + (col + c) * 4, y[p]);
             }
+        } else if (a.out_type == LQ_TOKEN_BF16) {
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+                if (in[p]) store_tok<true, 8>(out + p * 16 * L, y[p]);
+        } else {
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+                if (in[p]) store_tok<false, 8>(out + p * 32 * L, y[p]);
         }
+        x += a.step * a.x_stride;
+        second += a.step * a.second_stride;
+        if (!GATE) sum += a.step * a.sum_stride;
+        out += a.step * a.out_stride;
+        scale += a.step * a.scale_stride;
     }
 }
 
-// Workgroups: as many as the GPU holds at once, and rows in turn beyond that.
+// Workgroups: as many as the GPU holds at once, and tokens in turn beyond that.
 constexpr uint32_t MOST_GROUPS = 256 * 8;
 
 template <int L, int P, bool GATE>
-hipError_t launch(const RowArgs &a, bool xb, bool sb, hipStream_t st) {
+hipError_t launch(RowArgs a, bool xb, bool sb, hipStream_t st) {
     constexpr int threads = L > 256 ? L : 256, per = threads / L;
-    if (a.rows == 0) return hipSuccess;
-    const dim3 grid(std::min((a.rows - 1) / per + 1, MOST_GROUPS)), block(threads);
+    if (a.tokens == 0) return hipSuccess;
+    a.step = std::min(a.tokens, std::max(1u, MOST_GROUPS * per / a.heads_turn));
+    const dim3 grid((a.step * a.heads_turn - 1) / per + 1), block(threads);
     if (xb && sb) hipLaunchKernelGGL((rows_kernel<L, P, true, true, GATE>), grid, block, 0, st, a);
     else if (xb) hipLaunchKernelGGL((rows_kernel<L, P, true, false, GATE>), grid, block, 0, st, a);
     else if (sb) hipLaunchKernelGGL((rows_kernel<L, P, false, true, GATE>), grid, block, 0, st, a);
@@ -240,7 +280,7 @@ hipError_t launch_add_norm(const lq_add &n, hipStream_t st) {
     a.sum_stride = n.residual_out ? row_bytes(n.tokens, n.residual_out_stride, type_size(n.residual_dtype)) : 0;
     a.out_stride = row_bytes(n.tokens, n.out_stride, type_size(n.out_dtype));
     a.scale_stride = row_bytes(n.tokens, n.scale_stride, 1);
-    a.rows = (uint32_t)n.tokens;
+    a.tokens = (uint32_t)n.tokens;
     a.heads = a.heads_turn = 1;
     a.length = n.channels;
     a.norm = n.norm == LQ_NORM_RMS;
@@ -263,7 +303,7 @@ hipError_t launch_gate_norm(const lq_gated &g, hipStream_t st) {
     a.heads = (uint32_t)g.heads;
     // two heads of 64 share a block: a token's heads start at an even place
     a.heads_turn = g.d == 64 ? a.heads + (a.heads & 1) : a.heads;
-    a.rows = (uint32_t)g.tokens * a.heads_turn;
+    a.tokens = (uint32_t)g.tokens;
     a.length = g.d;
     a.norm = 1;
     a.out_type = g.out_dtype;

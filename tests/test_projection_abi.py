@@ -57,7 +57,7 @@ GATED = [
     (dict(dtype=2), EINVAL), (dict(gate_dtype=2), EINVAL), (dict(out_dtype=5), EINVAL), (dict(eps=-1.0), EINVAL), (dict(x=None), EINVAL),
     (dict(gate=None), EINVAL), (dict(out=None), EINVAL), (dict(scale=None), EINVAL), (dict(gate=GOOD + 8), EALIGN),
     (dict(weight=GOOD + 8), EALIGN), (dict(x_stride=380), EINVAL), (dict(gate_stride=388), EALIGN), (dict(out_stride=392), EALIGN),
-    (dict(scale_stride=2), EINVAL), (dict(tokens=(1 << 31) - 1, heads=2), EUNSUP), (dict(tokens=(1 << 30) + 1, heads=1, d=64), EUNSUP),
+    (dict(scale_stride=2), EINVAL), (dict(tokens=1 << 31), EUNSUP), (dict(heads=(1 << 20) + 1, x_stride=1 << 28), EUNSUP),
 ]
 WEIGHT = [
     (dict(n=0), EINVAL), (dict(k=0), EINVAL), (dict(k=264, w_stride=272), EUNSUP), (dict(dtype=2), EINVAL), (dict(w=None), EINVAL),
