@@ -361,6 +361,15 @@ def test_matmul_large(tokens, k, n):
     check_matmul(tokens, k, n, BF)
 
 
+@pytest.mark.parametrize("out", [BF, F32])
+@pytest.mark.parametrize("tokens,k,n", [(8200, 256, 2200), (8200, 128, 2200), (8192, 384, 2304), (40000, 256, 64), (30000, 640, 100),
+                                        (20000, 128, 200), (9000, 1024, 520), (8200, 144, 2200), (33, 256, 20000), (2100, 128, 2048)])
+def test_matmul_workgroups_that_take_several_tiles(tokens, k, n, out):
+    """More tiles than workgroups, whole ones and edges in turn, of one block of k and more (and one tile each where k ends
+    inside a block)."""
+    check_matmul(tokens, k, n, out, bias=n % 8 == 0)
+
+
 def test_matmul_values_that_are_not_finite_stay_in_their_row_and_channel():
     t, k, n = 70, 400, 300
     x, w = encoded(1, t, k), encoded(2, n, k)
