@@ -249,12 +249,13 @@ struct Tile {
     static_assert(TJ % 2 == 0 && TI % 2 == 0, "columns take turns in two registers, tiles of bf16 outputs go in pairs");
 };
 
-// Row m of a wave's tile i among its 16 TI rows of w, and the bits that place a row's pieces: they differ for the 8 pairs of
-// rows of a tile.
+// Row m of a wave's tile i among its 16 TI rows of w, and the bits that place a row's pieces: those of m / 2, as for the rows
+// of x.  (LDS serves a 16-byte read in groups of 16 lanes that take 8 rows of one lane group and the other 8 of the next; with
+// the bits of m / 2 in another order a fifth of the LDS's active cycles were conflicts.)
 template <bool EXACT>
 __device__ __forceinline__ int tile_row(int i, int m) { return EXACT ? 16 * i + m : 32 * (i >> 1) + 8 * (m >> 2) + 4 * (i & 1) + (m & 3); }
 template <bool EXACT>
-__device__ __forceinline__ int row_place(int row) { return EXACT ? row >> 1 & 7 : (row >> 3 & 3) | (row >> 1 & 1) << 2; }
+__device__ __forceinline__ int row_place(int row) { return EXACT ? row >> 1 & 7 : (row >> 3 & 3) << 1 | (row >> 1 & 1); }
 
 template <bool EXACT, int WT, int WC, int TJ, int TI, int STAGES>
 __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, int tiles_t, int tiles_c) {
