@@ -474,7 +474,7 @@ int32_t leapquant_scan_gates(const lq_dims *dims, const lq_scan *s, float *alpha
 #define LQ_ACT_SILU    0     /* z / (1 + exp(-z))                                    */
 #define LQ_ACT_SIGMOID 1     /* 1 / (1 + exp(-z))                                    */
 #define LQ_SCALE_BLOCK 128
-#define LQ_MAX_NORM_CHANNELS 32768
+#define LQ_MAX_NORM_CHANNELS 16384
 
 /*
  * leapquant_add_norm -- h = x + residual, residual_out = h, and
@@ -552,9 +552,9 @@ int32_t leapquant_quantize_weight(const lq_weight *w, void *stream);
  * the bits above 2^-13 of the largest: a sum is off by about 1.4e-5 of the sums' size
  * beside its rounding, at most 7 * 2^-13 of its terms where it cancels (take fp32
  * outputs where that matters; they run at about half the rate).  k is a multiple of
- * 16 up to 2^23, n any up to 2^26, tokens * n at most 2^36; rows of x and w are at
- * most 2^23 elements apart, rows of x_scale 2^20.  The order of sums is the same in every call
- * of the same sizes.
+ * 16 up to 2^23, n any up to 2^26, tokens are at most 2^28 and tokens * n 2^36; rows
+ * of x and w are at most 2^23 elements apart, rows of x_scale 2^20.  The order of sums
+ * is the same in every call of the same sizes.
  */
 typedef struct {
     int64_t tokens;

@@ -92,8 +92,11 @@ __device__ __forceinline__ void store4(const ProductArgs &a, int t, int c, f32x4
 // ---- few tokens -------------------------------------------------------------------
 //
 // Bound: HBM, the weight.  A workgroup owns 16 CT channels of 16 TT tokens; its waves take the blocks of k in turn, AHEAD
-// of them at a time, straight from memory into registers, and join their sums in LDS.
-template <bool EXACT, int TT, int CT, int WAVES, int AHEAD>
+// of them on their way, straight from memory into registers, and join their sums in LDS.  1 token x 4096 -> 12288 9.8 us (5.2 TB/s),
+// 77 x 1552 -> 1000 fp32 4.5.
+constexpr int WAVES = 8, AHEAD = 2;
+
+template <bool EXACT, int TT, int CT>
 __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs a) {
     __shared__ f32x4 parts[WAVES][TT * CT][64];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
@@ -150,8 +153,8 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs a) 
             }
         }
     };
-    // this wave's blocks, from a start of the workgroup's own on (rows of w are often a power of two apart: workgroups that
-    // read the same columns of many rows at once meet in a few memory channels); AHEAD of them are on their way
+    // This wave's blocks, from a start of the workgroup's own on: 1 token x 4096 -> 12288 13.0 -> 10.6 us, 4096 -> 4096 6.0 -> 4.9.
+    // (Why was not found: rows 128 bytes further apart change nothing, so it is not that rows meet in a few channels.)
     const int whole = a.k / BLOCK, start = whole ? (int)(blockIdx.x * 5u % (unsigned)whole) : 0;
     const int mine = wave < whole ? (whole - 1 - wave) / WAVES + 1 : 0;
     auto block = [&](int m) {
@@ -190,7 +193,7 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs a) 
 template <bool EXACT, int TT, int CT>
 hipError_t launch_few(const ProductArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)((a.n - 1) / (16 * CT) + 1), (unsigned)((a.tokens - 1) / (16 * TT) + 1));
-    hipLaunchKernelGGL((product_few_kernel<EXACT, TT, CT, 8, 2>), grid, dim3(512), 0, st, a);
+    hipLaunchKernelGGL((product_few_kernel<EXACT, TT, CT>), grid, dim3(64 * WAVES), 0, st, a);
     return hipGetLastError();
 }
 
@@ -200,7 +203,7 @@ hipError_t launch_few(const ProductArgs &a, hipStream_t st) {
 template <bool EXACT>
 hipError_t launch_few_tokens(const ProductArgs &a, hipStream_t st) {
     const int64_t t = (a.tokens - 1) / 16 + 1, c = (a.n - 1) / 16 + 1;
-    auto fits = [&](int tt, int ct) { return a.tokens > 4 && t >= tt && ((t + tt - 1) / tt) * ((c + ct - 1) / ct) >= 160; };
+    auto fits = [&](int tt, int ct) { return a.tokens > 4 && t >= tt && c >= ct && ((t + tt - 1) / tt) * ((c + ct - 1) / ct) >= 160; };
     if (fits(2, 4)) return launch_few<EXACT, 2, 4>(a, st);
     if (fits(2, 2)) return launch_few<EXACT, 2, 2>(a, st);
     if (fits(1, 4)) return launch_few<EXACT, 1, 4>(a, st);
@@ -210,11 +213,17 @@ hipError_t launch_few_tokens(const ProductArgs &a, hipStream_t st) {
 
 // ---- many tokens ------------------------------------------------------------------
 //
-// Bound: the matrix cores, with the LDS beside them.  A workgroup owns a tile of 16 WT TJ tokens x 16 WC TI channels, a wave
-// TJ x TI tiles of 16 x 16, all sums in registers.  Blocks of k are copied straight into LDS, STAGES - 1 ahead; a row's 8
-// pieces are placed by an exclusive or with bits of the row, so that the 16 rows that a read takes at once lie in 16 different
-// places of a 256-byte line of banks.  Channels are dealt to a wave's tiles so that a lane ends up with 16 bytes of
-// neighbouring outputs of a token at a time, and 4 lanes with 64.
+// Bound: issue, of matrix and vector instructions, which hardly overlap (of 32 + 8 cycles for a tile's products over a block
+// and the 4 sums a lane), with the waves meeting once a block; bytes for 256 tokens and less.  A workgroup owns a tile of
+// 16 WT TJ tokens x 16 WC TI channels, a wave TJ x TI tiles of 16 x 16, all sums in registers.  Blocks of k are copied straight
+// into LDS, STAGES - 1 ahead; a row's 8 pieces are placed by an exclusive or with bits of the row, so that the 16 rows that a
+// read takes at once lie in 16 different places of a 256-byte line of banks.  Channels are dealt to a wave's tiles so that a
+// lane ends up with 16 bytes of neighbouring outputs of a token at a time, and 4 lanes with 64.
+//
+// 8192 x 4096 -> 12288 bf16 396-412 us (2.0-2.1 PFLOP/s; the matrix cores are busy 51% of the cycles): without the outputs' stores
+// 376, without copies too 298-338, without the waves' meeting too 259 (a version before the last steps).  Two waves
+// a SIMD: one with twice the tile took 480.  256 x 4096 -> 12288 26 us; 1531 x 4096 -> 4096 fp32 59, where the
+// codes' conversions take as long as the products.
 __device__ const uint4 no_codes = {0, 0, 0, 0};
 
 // Copies into LDS as dma16's and dma_element's: 16 bytes per lane from a uniform base and a lane's offset, and one element.
@@ -267,7 +276,8 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
     const int wt = wave / WC, wc = wave % WC;
     const int whole = a.k / BLOCK, total = tiles_t * tiles_c;
 
-    // Workgroups go round the 8 XCDs: each gets neighbouring tiles, GROUP of tokens side by side, whose rows its L2 shares.
+    // Workgroups go round the 8 XCDs: each gets neighbouring tiles, GROUP of tokens side by side, whose rows its L2 shares, and
+    // starts an eighth of k further on (from 0 all of them: 8192 x 1024 -> 12288 142 instead of 126 us, 4096 -> 12288 440 and 418).
     struct Place {
         int t0, c0, start;
     };
@@ -277,9 +287,8 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
         const int band = id / (GROUP * tiles_c), first = band * GROUP, high = min(GROUP, tiles_t - first);
         const int in_band = id - band * GROUP * tiles_c;
         const int t = (first + in_band % high) * T::TOKENS, c = in_band / high * T::CHANNELS;
-        const int start = whole ? (int)((unsigned)(tiles_t > 1 ? xcd * whole / 8 : id * 5) % (unsigned)whole) : 0;
         // (divisions are made in vector registers)
-        return Place{__builtin_amdgcn_readfirstlane(t), __builtin_amdgcn_readfirstlane(c), __builtin_amdgcn_readfirstlane(start)};
+        return Place{__builtin_amdgcn_readfirstlane(t), __builtin_amdgcn_readfirstlane(c), (int)((int64_t)xcd * whole / 8)};
     };
 
     // ---- copies: the blocks of this workgroup's tiles, one after the other ----
@@ -304,7 +313,6 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
             wo[i] = (uint32_t)(min(8 * (wave * T::W_COPIES + i) + row8, a.n - 1 - at.c0) * a.w_stride) + piece_w(i);
         xbase = (uint64_t)(a.x + at.t0 * a.x_stride);
         wbase = (uint64_t)(a.w + at.c0 * a.w_stride);
-        kb = at.start;
         if (wave < T::TOKENS / 64) {
             sbase = (uint64_t)(a.xs + at.t0 * a.xs_stride);
             so = (uint32_t)(min(64 * wave + lane, a.tokens - 1 - at.t0) * a.xs_stride * 4);
@@ -312,6 +320,7 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
             sbase = (uint64_t)a.ws;
             so = (uint32_t)min(at.c0 / BLOCK + lane, (a.n - 1) / BLOCK) * (uint32_t)a.blocks * 4u;
         }
+        kb = at.start;
         to_copy = whole;
     };
     const uint32_t xl = lds_addr(codes) + wave * T::X_COPIES * 1024, wl = lds_addr(codes) + T::TOKENS * BLOCK + wave * T::W_COPIES * 1024;
@@ -369,7 +378,9 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
         if (j == 0) ws = scales[at][T::TOKENS + 16 * TI * wc / BLOCK];
     };
     int used = 0, stored = 0;       // blocks that were waited for; of the waits to come, how many have a tile's stores before them
+    // (the count of what is under way falls in the order of issue, loads and stores alike)
     constexpr int STORES = TJ * TI / (EXACT ? 1 : 2), LATER = T::COPIES * (STAGES - 2);
+    static_assert(LATER + STORES < 64, "a wait counts to 63");
     // the next block is here (and what was read before is in registers)
     auto meet = [&]() {
         ++used;

@@ -80,8 +80,8 @@ int32_t leapquant_matmul(const lq_matmul *m, void *stream) {
     int32_t e;
     if ((e = check_tokens(m->tokens)) != LQ_OK) return e;
     if (m->k % 16) return LQ_EUNSUPPORTED;
-    // (workgroups are counted in 32 bits with their work-items: 16 channels of few tokens, or at least 128 x 256 outputs)
-    if (m->n > 1 << 26 || m->tokens > (1LL << 36) / m->n) return LQ_EUNSUPPORTED;
+    // (a launch's work-items are counted in 32 bits: 512 of them for 16 channels of few tokens, for 128 x 128 outputs of many)
+    if (m->n > 1 << 26 || m->tokens > 1 << 28 || m->tokens > (1LL << 36) / m->n) return LQ_EUNSUPPORTED;
     // a tile's rows are addressed by 32 bits from its first one
     const int64_t T = m->tokens, apart = 1 << 23, scales_apart = 1 << 20;
     if (m->k > apart || (T > 1 && (m->x_stride > apart || m->x_scale_stride > scales_apart))) return LQ_EUNSUPPORTED;

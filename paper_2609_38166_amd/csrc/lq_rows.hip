@@ -3,8 +3,10 @@
 //   add_norm   h = x + residual,  y = h / sqrt(mean h^2 + eps) w
 //   gate_norm  y = x / sqrt(mean x^2 + eps) w act(gate), or the norm of x act(gate)
 //
-// Bound: HBM.  A lane owns 8 channels, so that a block of 128 is a row of 16 lanes (its largest magnitude by DPP); a row of
-// channels stays in the registers of 8 to 1024 lanes between its sum of squares and its output.
+// Bound: HBM; the gated norm's instructions come near it.  A lane owns 8 channels, so that a block of 128 is a row of 16 lanes
+// (its largest magnitude by DPP); a row of channels stays in the registers of 8 to 1024 lanes between its sum of squares and
+// its output.  bf16 to E4M3: add_norm of 8192 x 4096 48 us (4.9 TB/s), gate_norm of 8192 x 32 heads of 128 38-40 (4.3 TB/s; 290
+// vector instructions for 8 values a lane, 370 took 49-50).
 #include <algorithm>
 
 #include "lq_e4m3.hpp"
@@ -97,13 +99,13 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rows_kernel(RowArgs a) {
     float w[P][8];
     bool in[P];
 #pragma unroll
+    for (int p = 0; p < P; ++p) in[p] = there && 8 * (p * L + l) < a.length;
+#pragma unroll
     for (int p = 0; p < P; ++p) {
-        const int c = 8 * (p * L + l);
-        in[p] = there && c < a.length;
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[p][i] = 1.0f;
         if (a.weight && in[p]) {
-            const float4 *from = (const float4 *)(a.weight + (a.weight_heads ? col : 0) + c);
+            const float4 *from = (const float4 *)(a.weight + (a.weight_heads ? col : 0) + 8 * (p * L + l));
             const float4 u = from[0], v = from[1];
             w[p][0] = u.x; w[p][1] = u.y; w[p][2] = u.z; w[p][3] = u.w;
             w[p][4] = v.x; w[p][5] = v.y; w[p][6] = v.z; w[p][7] = v.w;
@@ -204,7 +206,8 @@ hipError_t launch(RowArgs a, bool xb, bool sb, hipStream_t st) {
     return hipGetLastError();
 }
 
-// Rows longer than the 32 lanes of a head: a wave, or a workgroup, with as many pieces a lane as it takes.
+// Rows longer than the 32 lanes of a head: a wave, or a workgroup, with as many pieces a lane as it takes (their
+// values, weights and loads are 40 registers each).
 template <bool GATE>
 hipError_t launch_long(const RowArgs &a, bool xb, bool sb, hipStream_t st) {
     if (a.length <= 512) return launch<64, 1, GATE>(a, xb, sb, st);
@@ -212,14 +215,13 @@ hipError_t launch_long(const RowArgs &a, bool xb, bool sb, hipStream_t st) {
     if (a.length <= 2048) return launch<64, 4, GATE>(a, xb, sb, st);
     if (a.length <= 4096) return launch<256, 2, GATE>(a, xb, sb, st);
     if (a.length <= 8192) return launch<256, 4, GATE>(a, xb, sb, st);
-    if (a.length <= 16384) return launch<1024, 2, GATE>(a, xb, sb, st);
-    return launch<1024, 4, GATE>(a, xb, sb, st);
+    return launch<1024, 2, GATE>(a, xb, sb, st);    // (LQ_MAX_NORM_CHANNELS)
 }
 
 // ---- weights --------------------------------------------------------------------
 //
-// A workgroup per block of 128 x 128, which stays in registers between its largest magnitude and its codes: 16 lanes a row
-// of the block, 16 rows at a time.
+// Bound: HBM.  A workgroup per block of 128 x 128, which stays in registers between its largest magnitude and its codes:
+// 16 lanes a row of the block, 16 rows at a time.  12288 x 4096 bf16 30 us (5.0 TB/s).
 struct WeightArgs {
     const char *w;
     char *out;

@@ -82,7 +82,7 @@ def outside_untouched(full, part_cols, start):
 
 # -------------------------------------------------------------------------------------------------------- add_norm
 
-CHANNELS = [8, 64, 120, 128, 136, 512, 520, 1024, 1544, 2048, 2056, 4096, 4104, 8192, 8200, 16384, 16392, 32768]
+CHANNELS = [8, 64, 120, 128, 136, 512, 520, 1024, 1544, 2048, 2056, 4096, 4104, 8192, 8200, 16376, 16384]
 
 
 @pytest.mark.parametrize("channels", CHANNELS)
@@ -205,7 +205,7 @@ def test_codes_reach_every_value():
 # ------------------------------------------------------------------------------------------------------- gate_norm
 
 @pytest.mark.parametrize("heads,d", [(1, 64), (3, 64), (4, 64), (1, 128), (5, 128), (32, 128), (3, 256), (2, 384), (3, 512),
-                                     (2, 1024), (1, 1664), (2, 2048), (1, 4096), (1, 8192), (1, 12288), (1, 32768)])
+                                     (2, 1024), (1, 1664), (2, 2048), (1, 4096), (1, 8192), (1, 12288), (2, 16384)])
 @pytest.mark.parametrize("dtype,gtype,out,act,first,weight", [
     (BF, BF, E4, "silu", False, 1), (F32, BF, E4, "sigmoid", False, 1), (F32, F32, F32, "silu", True, 2),
     (BF, F32, BF, "sigmoid", True, 0), (BF, BF, E4, "silu", True, 2)])

@@ -42,7 +42,7 @@ def product(**kw):
 
 ADD = [
     (dict(tokens=-1), EINVAL), (dict(tokens=1 << 31), EUNSUP), (dict(channels=0), EINVAL), (dict(channels=-8), EINVAL),
-    (dict(channels=252), EUNSUP), (dict(channels=32776, x_stride=40000), EUNSUP), (dict(norm=B.LQ_NORM_L2), EINVAL),
+    (dict(channels=252), EUNSUP), (dict(channels=16392, x_stride=20000), EUNSUP), (dict(norm=B.LQ_NORM_L2), EINVAL),
     (dict(norm=3), EINVAL), (dict(norm=B.LQ_NORM_NONE), EINVAL), (dict(dtype=2), EINVAL), (dict(residual_dtype=2), EINVAL),
     (dict(out_dtype=3), EINVAL), (dict(out_dtype=-1), EINVAL), (dict(eps=-1.0), EINVAL), (dict(eps=float("nan")), EINVAL),
     (dict(eps=float("inf")), EINVAL), (dict(x=None), EINVAL), (dict(out=None), EINVAL), (dict(scale=None), EINVAL),
@@ -53,7 +53,7 @@ ADD = [
 ]
 GATED = [
     (dict(tokens=-1), EINVAL), (dict(heads=0), EINVAL), (dict(d=0), EINVAL), (dict(d=32), EUNSUP), (dict(d=192), EUNSUP),
-    (dict(d=32896, x_stride=1 << 17), EUNSUP), (dict(act=2), EINVAL), (dict(gate_first=2), EINVAL), (dict(weight_heads=-1), EINVAL),
+    (dict(d=16512, x_stride=1 << 17), EUNSUP), (dict(act=2), EINVAL), (dict(gate_first=2), EINVAL), (dict(weight_heads=-1), EINVAL),
     (dict(dtype=2), EINVAL), (dict(gate_dtype=2), EINVAL), (dict(out_dtype=5), EINVAL), (dict(eps=-1.0), EINVAL), (dict(x=None), EINVAL),
     (dict(gate=None), EINVAL), (dict(out=None), EINVAL), (dict(scale=None), EINVAL), (dict(gate=GOOD + 8), EALIGN),
     (dict(weight=GOOD + 8), EALIGN), (dict(x_stride=380), EINVAL), (dict(gate_stride=388), EALIGN), (dict(out_stride=392), EALIGN),
