@@ -220,7 +220,7 @@ hipError_t launch_few_tokens(const ProductArgs &a, hipStream_t st) {
 // read takes at once lie in 16 different places of a 256-byte line of banks.  Channels are dealt to a wave's tiles so that a
 // lane ends up with 16 bytes of neighbouring outputs of a token at a time, and 4 lanes with 64.
 //
-// 8192 x 4096 -> 12288 bf16 396-412 us (2.0-2.1 PFLOP/s; the matrix cores are busy 51% of the cycles): without the outputs' stores
+// 8192 x 4096 -> 12288 bf16 385-400 us (2.1 PFLOP/s; the matrix cores are busy 51% of the cycles): without the outputs' stores
 // 376, without copies too 298-338, without the waves' meeting too 259 (a version before the last steps).  Two waves
 // a SIMD: one with twice the tile took 480.  256 x 4096 -> 12288 26 us; 1531 x 4096 -> 4096 fp32 59, where the
 // codes' conversions take as long as the products.
@@ -276,19 +276,20 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
     const int wt = wave / WC, wc = wave % WC;
     const int whole = a.k / BLOCK, total = tiles_t * tiles_c;
 
-    // Workgroups go round the 8 XCDs: each gets neighbouring tiles, GROUP of tokens side by side, whose rows its L2 shares, and
-    // starts an eighth of k further on (from 0 all of them: 8192 x 1024 -> 12288 142 instead of 126 us, 4096 -> 12288 440 and 418).
+    // Workgroups go round the 8 XCDs: each gets neighbouring tiles, a band of GROUP tiles of tokens side by side, whose rows its
+    // L2 shares.  Bands start an eighth of the channels apart: where all XCDs walked the weight's rows alike, 8192 x 1024 ->
+    // 12288 took 142 instead of 126 us, 4096 -> 12288 440 and 400.
     struct Place {
-        int t0, c0, start;
+        int t0, c0;
     };
     auto place = [&](int turn) {
         constexpr int GROUP = 4;
         const int xcd = turn % 8, id = xcd * (total / 8) + min(xcd, total % 8) + turn / 8;
         const int band = id / (GROUP * tiles_c), first = band * GROUP, high = min(GROUP, tiles_t - first);
         const int in_band = id - band * GROUP * tiles_c;
-        const int t = (first + in_band % high) * T::TOKENS, c = in_band / high * T::CHANNELS;
+        const int t = (first + in_band % high) * T::TOKENS, c = (in_band / high + band * (tiles_c / 8)) % tiles_c * T::CHANNELS;
         // (divisions are made in vector registers)
-        return Place{__builtin_amdgcn_readfirstlane(t), __builtin_amdgcn_readfirstlane(c), (int)((int64_t)xcd * whole / 8)};
+        return Place{__builtin_amdgcn_readfirstlane(t), __builtin_amdgcn_readfirstlane(c)};
     };
 
     // ---- copies: the blocks of this workgroup's tiles, one after the other ----
@@ -320,7 +321,7 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
             sbase = (uint64_t)a.ws;
             so = (uint32_t)min(at.c0 / BLOCK + lane, (a.n - 1) / BLOCK) * (uint32_t)a.blocks * 4u;
         }
-        kb = at.start;
+        kb = 0;
         to_copy = whole;
     };
     const uint32_t xl = lds_addr(codes) + wave * T::X_COPIES * 1024, wl = lds_addr(codes) + T::TOKENS * BLOCK + wave * T::W_COPIES * 1024;
@@ -340,7 +341,7 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
         }
     };
     auto copy_done = [&]() {
-        kb = kb + 1 == whole ? 0 : kb + 1;
+        ++kb;
         --to_copy;
         place_of_copy = place_of_copy + 1 == STAGES ? 0 : place_of_copy + 1;
     };
