@@ -224,8 +224,6 @@ hipError_t launch_few_tokens(const ProductArgs &a, hipStream_t st) {
 // 376, without copies too 298-338, without the waves' meeting too 259 (a version before the last steps).  Two waves
 // a SIMD: one with twice the tile took 480.  256 x 4096 -> 12288 26 us; 1531 x 4096 -> 4096 fp32 59, where the
 // codes' conversions take as long as the products.
-__device__ const uint4 no_codes = {0, 0, 0, 0};
-
 // Copies into LDS as dma16's and dma_element's: 16 bytes per lane from a uniform base and a lane's offset, and one element.
 // Nothing is copied where `left` is not positive: no lane is on then (all are where these are called).  By the mask and
 // not by a branch, so that the products around them stay one run of instructions.
@@ -322,7 +320,7 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
             so = (uint32_t)min(at.c0 / BLOCK + lane, (a.n - 1) / BLOCK) * (uint32_t)a.blocks * 4u;
         }
         kb = 0;
-        to_copy = whole;
+        to_copy = a.blocks;
     };
     const uint32_t xl = lds_addr(codes) + wave * T::X_COPIES * 1024, wl = lds_addr(codes) + T::TOKENS * BLOCK + wave * T::W_COPIES * 1024;
     const uint32_t sl = lds_addr(scales) + 256 * min(wave, T::TOKENS / 64);
@@ -340,16 +338,45 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
                 dma4_if(left, sbase + (uint64_t)kb * 4, so, sl + place_of_copy * (T::SCALES * 4));
         }
     };
+    // The last block, where k ends inside it, all at once: zeros past k, in places that nobody reads any more.  (Each row has
+    // pieces before k, so every copy has lanes and is counted.)
+    auto copy_short = [&]() {
+        const int end = a.k - whole * BLOCK, st = place_of_copy;
+        const uint4 zero = make_uint4(0, 0, 0, 0);
+        const char *x = (const char *)xbase + whole * BLOCK, *w = (const char *)wbase + whole * BLOCK;
+        char *xz = codes[st] + wave * T::X_COPIES * 1024 + 16 * lane, *wz = codes[st] + (T::TOKENS * BLOCK + wave * T::W_COPIES * 1024) + 16 * lane;
+#pragma unroll
+        for (int i = 0; i < T::X_COPIES; ++i) {
+            const uint32_t to = __builtin_amdgcn_readfirstlane(xl + st * T::STAGE + 1024 * i);
+            if (piece_x(i) < end) dma16(x + xo[i], to);
+            else *(uint4 *)(xz + 1024 * i) = zero;
+        }
+#pragma unroll
+        for (int i = 0; i < T::W_COPIES; ++i) {
+            const uint32_t to = __builtin_amdgcn_readfirstlane(wl + st * T::STAGE + 1024 * i);
+            if (piece_w(i) < end) dma16(w + wo[i], to);
+            else *(uint4 *)(wz + 1024 * i) = zero;
+        }
+        dma4_if(1, sbase + (uint64_t)kb * 4, so, sl + st * (T::SCALES * 4));
+    };
     auto copy_done = [&]() {
         ++kb;
         --to_copy;
         place_of_copy = place_of_copy + 1 == STAGES ? 0 : place_of_copy + 1;
     };
-    auto copy = [&]() {
+    // Before a block's parts: how many blocks are left, 0 if there is nothing to send in parts.
+    auto copy_begin = [&]() {
         next_tile();
-        copied += to_copy > 0;
+        if (to_copy <= 0) return 0;
+        ++copied;
+        if (kb < whole) return to_copy;
+        copy_short();
+        return 0;
+    };
+    auto copy = [&]() {
+        const int left = copy_begin();
 #pragma unroll
-        for (int part = 0; part < T::PARTS; ++part) copy_part(to_copy, part);
+        for (int part = 0; part < T::PARTS; ++part) copy_part(left, part);
         copy_done();
     };
 
@@ -389,7 +416,7 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
         --stored;
         __syncthreads();
     };
-    auto multiply = [&](int at, int next, bool ahead, int left) {
+    auto multiply = [&](int at, int next, int left) {
         f32x4 part[3];
         float scale[2], wsb = ws;
         Operand<EXACT> w[TI], x;
@@ -403,15 +430,15 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
                 x.set(xraw[j & 1][0], xraw[j & 1][1]);
                 if (j + 1 < TJ) {
                     read_x(at, j + 1);
-                } else if (ahead) {
+                } else {
                     meet();
                     read_x(next, 0);
                 }
             }
-            if (ahead && q < TI * TJ && i == 1 && j < T::PARTS) copy_part(left, j);
+            if (q < TI * TJ && i == 1 && j < T::PARTS) copy_part(left, j);
             if (q < TI * TJ) part[q % 3] = block_product(w[i], x);
             __builtin_amdgcn_sched_barrier(0);
-            if (ahead && q < TI * TJ && j == TJ - 1) read_w(next, i);
+            if (q < TI * TJ && j == TJ - 1) read_w(next, i);
             if (q > 1) {
                 const int jw = (q - 2) / TI, iw = (q - 2) % TI;
 #pragma unroll
@@ -419,11 +446,6 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-    };
-    auto begin = [&](int at) {
-        read_x(at, 0);
-#pragma unroll
-        for (int i = 0; i < TI; ++i) read_w(at, i);
     };
     auto clear = [&]() {
 #pragma unroll
@@ -463,64 +485,35 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
 
     int here = 0;                   // place in LDS of the block at hand
     bool sent = false;              // whether the copies that go with the block at hand were sent before
-    if (whole > 0) {
 #pragma unroll
-        for (int b = 0; b < STAGES - 1; ++b) copy();
-        meet();
-        begin(0);
-    }
+    for (int b = 0; b < STAGES - 1; ++b) copy();
+    meet();
+    read_x(0, 0);
+#pragma unroll
+    for (int i = 0; i < TI; ++i) read_w(0, i);
     for (int mine = blockIdx.x; mine < total; mine += gridDim.x) {
         const Place tile = place(mine);
         clear();
-        for (int b = 0; b < whole; ++b) {
-            int left = 0;
-            if (!sent) {
-                next_tile();
-                left = to_copy;
-                copied += to_copy > 0;
-            }
+        for (int b = 0; b < a.blocks; ++b) {
+            const int left = sent ? 0 : copy_begin();
             const int next = here + 1 == STAGES ? 0 : here + 1;
-            multiply(here, next, true, left);       // (after the last block it reads what lies there, for nobody)
+            multiply(here, next, left);             // (after the last block it reads what lies there, for nobody)
             if (!sent) copy_done();
             sent = false;
             here = next;
         }
-        if (whole < a.blocks) {             // a last block that is shorter: zeros past k (the grid has a workgroup a tile then)
-            Place at = tile;
-            asm volatile("" : "+s"(at.t0), "+s"(at.c0));    // (addresses are made here, not kept through the loop above)
-            const int left = a.k - whole * BLOCK;
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < T::X_COPIES; ++i) {
-                const int64_t row = min(at.t0 + 8 * (wave * T::X_COPIES + i) + row8, a.tokens - 1);
-                const char *from = a.x + row * a.x_stride + whole * BLOCK + piece_x(i);
-                dma16(piece_x(i) < left ? from : (const char *)&no_codes, xl + 1024 * i);
-            }
-#pragma unroll
-            for (int i = 0; i < T::W_COPIES; ++i) {
-                const int64_t row = min(at.c0 + 8 * (wave * T::W_COPIES + i) + row8, a.n - 1);
-                const char *from = a.w + row * a.w_stride + whole * BLOCK + piece_w(i);
-                dma16(piece_w(i) < left ? from : (const char *)&no_codes, wl + 1024 * i);
-            }
-            dma_element<4>((wave < T::TOKENS / 64 ? a.xs + min(at.t0 + 64 * wave + lane, a.tokens - 1) * a.xs_stride
-                                                  : a.ws + (int64_t)min(at.c0 / BLOCK + lane, (a.n - 1) / BLOCK) * a.blocks) + whole, sl);
-            wait_vm_all();
-            __syncthreads();
-            begin(0);
-            multiply(0, 0, false, 0);
-        }
-        if (whole > 0) copy();              // ahead of the outputs, which the next blocks then need not wait for
+        copy();                     // ahead of the outputs, which the next blocks then need not wait for
         sent = true;
         store(tile);
     }
 }
 
-// Workgroups: one for each CU, which takes tiles in turn; one a tile where k ends inside a block.
+// Workgroups: one for each CU, which takes tiles in turn.
 template <bool EXACT, int WT, int WC, int TJ, int TI, int STAGES>
 hipError_t launch_tiles(const ProductArgs &a, hipStream_t st) {
     using T = Tile<WT, WC, TJ, TI, STAGES>;
     const int tiles_t = (a.tokens - 1) / T::TOKENS + 1, tiles_c = (a.n - 1) / T::CHANNELS + 1, total = tiles_t * tiles_c;
-    const dim3 grid((unsigned)(a.k % BLOCK ? total : std::min(total, 256))), block(64 * T::WAVES);
+    const dim3 grid((unsigned)std::min(total, 256)), block(64 * T::WAVES);
     hipLaunchKernelGGL((product_kernel<EXACT, WT, WC, TJ, TI, STAGES>), grid, block, 0, st, a, tiles_t, tiles_c);
     return hipGetLastError();
 }
