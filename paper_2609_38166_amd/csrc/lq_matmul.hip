@@ -213,17 +213,18 @@ hipError_t launch_few_tokens(const ProductArgs &a, hipStream_t st) {
 
 // ---- many tokens ------------------------------------------------------------------
 //
-// Bound: issue, of matrix and vector instructions, which hardly overlap (of 32 + 8 cycles for a tile's products over a block
-// and the 4 sums a lane), with the waves meeting once a block; bytes for 256 tokens and less.  A workgroup owns a tile of
+// Bound: issue, of matrix and vector instructions, which hardly overlap (32 cycles for a tile's products over a block, 8 for
+// its 4 sums a lane), and the waves' meeting once a block; bytes for 256 tokens and less.  A workgroup owns a tile of
 // 16 WT TJ tokens x 16 WC TI channels, a wave TJ x TI tiles of 16 x 16, all sums in registers.  Blocks of k are copied straight
 // into LDS, STAGES - 1 ahead; a row's 8 pieces are placed by an exclusive or with bits of the row, so that the 16 rows that a
 // read takes at once lie in 16 different places of a 256-byte line of banks.  Channels are dealt to a wave's tiles so that a
 // lane ends up with 16 bytes of neighbouring outputs of a token at a time, and 4 lanes with 64.
 //
-// 8192 x 4096 -> 12288 bf16 385-400 us (2.1 PFLOP/s; the matrix cores are busy 51% of the cycles): without the outputs' stores
+// 8192 x 4096 -> 12288 bf16 381-396 us (2.1 PFLOP/s; the matrix cores are busy 53% of the cycles): without the outputs' stores
 // 376, without copies too 298-338, without the waves' meeting too 259 (a version before the last steps).  Two waves
 // a SIMD: one with twice the tile took 480.  256 x 4096 -> 12288 26 us; 1531 x 4096 -> 4096 fp32 59, where the
 // codes' conversions take as long as the products.
+
 // Copies into LDS as dma16's and dma_element's: 16 bytes per lane from a uniform base and a lane's offset, and one element.
 // Nothing is copied where `left` is not positive: no lane is on then (all are where these are called).  By the mask and
 // not by a branch, so that the products around them stay one run of instructions.

@@ -5,7 +5,7 @@
 //
 // Bound: HBM; the gated norm's instructions come near it.  A lane owns 8 channels, so that a block of 128 is a row of 16 lanes
 // (its largest magnitude by DPP); a row of channels stays in the registers of 8 to 1024 lanes between its sum of squares and
-// its output.  bf16 to E4M3: add_norm of 8192 x 4096 48 us (4.9 TB/s), gate_norm of 8192 x 32 heads of 128 38-40 (4.3 TB/s; 290
+// its output.  bf16 to E4M3: add_norm of 8192 x 4096 48 us (4.9 TB/s), gate_norm of 8192 x 32 heads of 128 37-38 (4.5 TB/s; 290
 // vector instructions for 8 values a lane, 370 took 49-50).
 #include <algorithm>
 
