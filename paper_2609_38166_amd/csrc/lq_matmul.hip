@@ -222,7 +222,7 @@ hipError_t launch_few_tokens(const ProductArgs &a, hipStream_t st) {
 //
 // 8192 x 4096 -> 12288 bf16 380-418 us (2.1 PFLOP/s; the matrix cores are busy 55% of the cycles): without the outputs' stores
 // 376, without copies too 298-338, without the waves' meeting too 259 (a version before the last steps).  Two waves
-// a SIMD: one with twice the tile took 480.  256 x 4096 -> 12288 24 us; 1531 x 4096 -> 4096 fp32 61, where the
+// a SIMD: one with twice the tile took 480.  256 x 4096 -> 12288 24 us; 1531 x 4096 -> 4096 fp32 55, where the
 // codes' conversions take as long as the products.
 
 // Copies into LDS as dma16's and dma_element's: 16 bytes per lane from a uniform base and a lane's offset, and one element.
@@ -522,17 +522,19 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-// The tile whose rounds of 256 workgroups take the least time; a round's, for k = 4096, was measured (in 0.1 us).
+// The tile whose rounds of 256 workgroups take the least time; a round's, for k = 4096, was measured (in 0.1 us).  192 tokens
+// fill rounds that 128 and 256 do not: 1531 x 4096 -> 4096 fp32 61 -> 55 us (256 tiles instead of 192 larger ones), 1536 x 4096 -> 8192
+// fp32 118 -> 89, 3000 x 4096 -> 4096 bf16 70 -> 65.
 template <bool EXACT>
 hipError_t launch_many_tokens(const ProductArgs &a, hipStream_t st) {
     struct Choice {
         int tokens, channels, round;
     };
-    constexpr Choice choices[] = {{64, 64, EXACT ? 222 : 153}, {64, 128, EXACT ? 275 : 189}, {128, 128, EXACT ? 424 : 258},
-                                  {128, 256, EXACT ? 644 : 408}, {256, 256, 655}};
+    constexpr Choice choices[] = {{64, 64, EXACT ? 222 : 150}, {64, 128, EXACT ? 295 : 195}, {128, 128, EXACT ? 412 : 270}, {192, 128, EXACT ? 552 : 358},
+                                  {128, 256, EXACT ? 645 : 415}, {192, 256, EXACT ? 880 : 640}, {256, 256, 745}};
     int best = 0;
     int64_t least = INT64_MAX;
-    for (int i = 0; i < (EXACT ? 4 : 5); ++i) {
+    for (int i = 0; i < (EXACT ? 6 : 7); ++i) {
         const int64_t tiles = (int64_t)((a.tokens - 1) / choices[i].tokens + 1) * ((a.n - 1) / choices[i].channels + 1);
         const int64_t time = (tiles + 255) / 256 * choices[i].round;
         if (time <= least) best = i, least = time;
@@ -541,7 +543,9 @@ hipError_t launch_many_tokens(const ProductArgs &a, hipStream_t st) {
         case 0: return launch_tiles<EXACT, 2, 2, 2, 2, 4>(a, st);
         case 1: return launch_tiles<EXACT, 2, 4, 2, 2, 3>(a, st);
         case 2: return launch_tiles<EXACT, 2, 4, 4, 2, 4>(a, st);
-        case 3: return launch_tiles<EXACT, 2, 4, 4, 4, 3>(a, st);
+        case 3: return launch_tiles<EXACT, 2, 4, 6, 2, 3>(a, st);
+        case 4: return launch_tiles<EXACT, 2, 4, 4, 4, 3>(a, st);
+        case 5: return launch_tiles<EXACT, 2, 4, 6, 4, 2>(a, st);
         default: return launch_tiles<false, 2, 4, 8, 4, 2>(a, st);      // (bf16 only: twice the registers for fp32)
     }
 }

@@ -370,6 +370,14 @@ def test_matmul_workgroups_that_take_several_tiles(tokens, k, n, out):
     check_matmul(tokens, k, n, out, bias=n % 8 == 0)
 
 
+@pytest.mark.parametrize("out", [BF, F32])
+@pytest.mark.parametrize("tokens,k,n", [(1531, 272, 4096), (1530, 144, 4093), (8084, 400, 1291), (3000, 272, 4096), (4381, 144, 5380),
+                                        (1924, 400, 8850), (2050, 144, 7196), (8234, 272, 779), (7684, 144, 3100)])
+def test_matmul_tiles(tokens, k, n, out):
+    """Every size of tile, with one tile a workgroup and with two, whole ones and edges."""
+    check_matmul(tokens, k, n, out, bias=n % 2 == 1)
+
+
 def test_matmul_values_that_are_not_finite_stay_in_their_row_and_channel():
     t, k, n = 70, 400, 300
     x, w = encoded(1, t, k), encoded(2, n, k)
