@@ -220,7 +220,7 @@ hipError_t launch_few_tokens(const ProductArgs &a, hipStream_t st) {
 // read takes at once lie in 16 different places of a 256-byte line of banks.  Channels are dealt to a wave's tiles so that a
 // lane ends up with 16 bytes of neighbouring outputs of a token at a time, and 4 lanes with 64.
 //
-// 8192 x 4096 -> 12288 bf16 380-418 us (2.1 PFLOP/s; the matrix cores are busy 55% of the cycles): without the outputs' stores
+// 8192 x 4096 -> 12288 bf16 380-385 us (2.1 PFLOP/s; the matrix cores are busy 55% of the cycles): without the outputs' stores
 // 376, without copies too 298-338, without the waves' meeting too 259 (a version before the last steps).  Two waves
 // a SIMD: one with twice the tile took 480.  256 x 4096 -> 12288 24 us; 1531 x 4096 -> 4096 fp32 55, where the
 // codes' conversions take as long as the products.
