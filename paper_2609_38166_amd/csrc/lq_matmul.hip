@@ -67,6 +67,13 @@ __device__ __forceinline__ f32x4 block_product(const Operand<true> &w, const Ope
     return p;
 }
 
+// 16 codes of a row, zeros past its end (loaded from within and then cleared: a choice between the row and a constant would be
+// one between addresses, with the constant in scratch memory).
+__device__ __forceinline__ uint4 piece(const char *row, int at, int k) {
+    const uint4 v = *(const uint4 *)(row + min(at, k - 16));
+    return at < k ? v : make_uint4(0, 0, 0, 0);
+}
+
 // 4 neighbouring channels of a token, from channel c on (rows start at multiples of 16 bytes).
 __device__ __forceinline__ void store4(const ProductArgs &a, int t, int c, f32x4 v) {
     if (t >= a.tokens || c >= a.n) return;
@@ -121,9 +128,8 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs a) 
     auto load = [&](Pieces &o, int b, bool whole) {
         const int at = b * BLOCK + 16 * g;
         auto pieces = [&](const char *row, uint4 *p) {
-            const uint4 none = make_uint4(0, 0, 0, 0);
-            p[0] = whole || at < a.k ? *(const uint4 *)(row + at) : none;
-            p[1] = whole || at + 64 < a.k ? *(const uint4 *)(row + at + 64) : none;
+            p[0] = whole ? *(const uint4 *)(row + at) : piece(row, at, a.k);
+            p[1] = whole ? *(const uint4 *)(row + at + 64) : piece(row, at + 64, a.k);
         };
 #pragma unroll
         for (int i = 0; i < CT; ++i) {
@@ -137,16 +143,17 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs a) 
         }
     };
     auto add = [&](const Pieces &o) {
-        Operand<EXACT> w[CT];
+        // (x's operands are kept and the weight's made one at a time: the other way 2 x 4 tiles of fp32 spilled registers)
+        Operand<EXACT> x[TT];
 #pragma unroll
-        for (int i = 0; i < CT; ++i) w[i].set(o.w[i][0], o.w[i][1]);
+        for (int j = 0; j < TT; ++j) x[j].set(o.x[j][0], o.x[j][1]);
 #pragma unroll
-        for (int j = 0; j < TT; ++j) {
-            Operand<EXACT> x;
-            x.set(o.x[j][0], o.x[j][1]);
+        for (int i = 0; i < CT; ++i) {
+            Operand<EXACT> w;
+            w.set(o.w[i][0], o.w[i][1]);
 #pragma unroll
-            for (int i = 0; i < CT; ++i) {
-                const f32x4 p = block_product(w[i], x);
+            for (int j = 0; j < TT; ++j) {
+                const f32x4 p = block_product(w, x[j]);
                 const float f = o.s[j] * o.ws[i];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(p[r], f, acc[i][j][r]);
