@@ -551,7 +551,10 @@ int32_t leapquant_quantize_weight(const lq_weight *w, void *stream);
  * outputs come from the matrix cores' 8-bit products, which keep of every 8 products
  * the bits above 2^-13 of the largest: a sum is off by about 1.4e-5 of the sums' size
  * beside its rounding, at most 7 * 2^-13 of its terms where it cancels (take fp32
- * outputs where that matters; they run at about half the rate).  k is a multiple of
+ * outputs where that matters; they run at about half the rate).  Scales are any fp32
+ * numbers: where fp32 does not hold the product of two as a normal number they are
+ * applied apart, so nothing is lost but what a sum itself cannot hold (calls with such
+ * scales may take 10 to 20 times as long).  k is a multiple of
  * 16 up to 2^23, n any up to 2^26, tokens are at most 2^28 and tokens * n 2^36; rows
  * of x and w are at most 2^23 elements apart, rows of x_scale 2^20.  The order of sums
  * is the same in every call of the same sizes.

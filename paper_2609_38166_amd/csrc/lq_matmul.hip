@@ -74,6 +74,86 @@ __device__ __forceinline__ uint4 piece(const char *row, int at, int k) {
     return at < k ? v : make_uint4(0, 0, 0, 0);
 }
 
+// ---- scales whose product fp32 does not hold -----------------------------------------
+//
+// x_scale * w_scale may be 0, denormal or infinite where with the block's sum it is a normal number.  The kernels multiply
+// the scales first, in 32 bits, and keep the least product.  A wave whose least one is below the normal numbers, or whose sums
+// are not finite (one channel of a token tells: an infinite product leaves none of them so), looks its scales over, and if there
+// are such products it makes its tiles again, straight from memory, with these as mantissas and exponents apart.  The other
+// products keep their bits: the same instructions in the same order.  (Making up for it in the loops cost the larger tiles
+// their registers, masks of the lanes 1 to 18% of the time; the least product costs half an instruction a column.)
+constexpr int ZERO = 0x060, DENORMAL = 0x090, NORMAL = 0x108, ANY = 0x3FF;
+__device__ __forceinline__ bool is(float x, int classes) { return __builtin_amdgcn_classf(x, classes); }
+__device__ __forceinline__ bool beyond(float xs, float ws) {
+    return is(xs * ws, ANY - NORMAL) && is(xs, NORMAL | DENORMAL) && is(ws, NORMAL | DENORMAL);
+}
+
+// What that rare path needs, read anew where it begins: the kernel's arguments from memory and the lane from a count of lanes, so
+// that nothing of them takes registers in the loops before (the path comes after all tiles for the same reason: behind each
+// tile's stores some 30 more scalar registers were spilled).
+struct Anew {
+    ProductArgs a;
+    int lane;
+    __device__ __forceinline__ Anew() {
+        auto p = (const ProductArgs *)__builtin_amdgcn_kernarg_segment_ptr();       // (the first argument)
+        uint32_t all = ~0u;
+        asm volatile("" : "+s"(p), "+s"(all));
+        a = *p;
+        lane = (int)__builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0u));
+    }
+};
+
+// Whether a lane has such a product: lane l16 looks at token t + l16, the lane groups at every fourth block of k each.  Rows of
+// zeros, as padded batches have them, lose nothing by a product that is too small.
+__device__ __forceinline__ bool any_beyond(const Anew &n, int t, int wb) {
+    const ProductArgs &a = n.a;
+    t = min(t + (n.lane & 15), a.tokens - 1);
+    const float *xs = a.xs + t * a.xs_stride, *ws = a.ws + min(wb, (a.n - 1) / BLOCK) * a.blocks;
+    const char *x = a.x + t * a.x_stride;
+    bool found = false;
+#pragma unroll 4
+    for (int b = n.lane >> 4; b < a.blocks; b += 4) {
+        if (!beyond(xs[b], ws[b])) continue;
+        uint32_t any = fabsf(xs[b] * ws[b]) > 1.0f;
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) {
+            const uint4 v = piece(x, b * BLOCK + 16 * i, a.k);
+            any |= (v.x | v.y | v.z | v.w) & 0x7F7F7F7Fu;
+        }
+        found |= any != 0;
+    }
+    return __builtin_amdgcn_ballot_w64(found) != 0;
+}
+
+// A tile of 16 x 16: lane l16 takes token t and row `row` of w, whose scales are those of block `wb` of rows.  Adds blocks first,
+// first + step, ... to sum, `count` of them, counted round at `wrap`.
+template <bool EXACT>
+__device__ __forceinline__ f32x4 tile_apart(const Anew &n, int t, int row, int wb, int first, int step, int count, int wrap, f32x4 sum) {
+    const ProductArgs &a = n.a;
+    const int g = n.lane >> 4;
+    t = min(t, a.tokens - 1);
+    const char *x = a.x + t * a.x_stride, *w = a.w + min(row, a.n - 1) * a.w_stride;
+    const float *xs = a.xs + t * a.xs_stride, *ws = a.ws + min(wb, (a.n - 1) / BLOCK) * a.blocks;
+#pragma unroll 1
+    for (int m = 0; m < count; ++m) {
+        int b = first + m * step;
+        if (b >= wrap) b -= wrap;
+        const int at = b * BLOCK + 16 * g;
+        Operand<EXACT> wo, xo;
+        wo.set(piece(w, at, a.k), piece(w, at + 64, a.k));
+        xo.set(piece(x, at, a.k), piece(x, at + 64, a.k));
+        const f32x4 p = block_product(wo, xo);
+        const float s = xs[b], u = ws[b], f = s * u;
+        const bool apart = beyond(s, u);
+        const float mantissa = __builtin_amdgcn_frexp_mantf(s) * __builtin_amdgcn_frexp_mantf(u);
+        const int exponent = __builtin_amdgcn_frexp_expf(s) + __builtin_amdgcn_frexp_expf(u);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            sum[r] = apart ? sum[r] + __builtin_amdgcn_ldexpf(p[r] * mantissa, exponent) : fmaf(p[r], f, sum[r]);
+    }
+    return sum;
+}
+
 // 4 neighbouring channels of a token, from channel c on (rows start at multiples of 16 bytes).
 __device__ __forceinline__ void store4(const ProductArgs &a, int t, int c, f32x4 v) {
     if (t >= a.tokens || c >= a.n) return;
@@ -120,6 +200,7 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs a) 
         srow[j] = a.xs + t * a.xs_stride;
     }
     f32x4 acc[CT][TT] = {};
+    float low = 1.0f;               // the least product of scales
     struct Pieces {
         uint4 w[CT][2], x[TT][2];
         float ws[CT], s[TT];
@@ -155,6 +236,7 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs a) 
             for (int j = 0; j < TT; ++j) {
                 const f32x4 p = block_product(w, x[j]);
                 const float f = o.s[j] * o.ws[i];
+                low = fminf(low, fabsf(f));
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(p[r], f, acc[i][j][r]);
             }
@@ -183,10 +265,33 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs a) 
         load(o[0], whole, false);
         add(o[0]);
     }
+    bool again = is(low, ANY - NORMAL);
 #pragma unroll
     for (int i = 0; i < CT; ++i)
 #pragma unroll
-        for (int j = 0; j < TT; ++j) parts[wave][i * TT + j][lane] = acc[i][j];
+        for (int j = 0; j < TT; ++j) again |= !is(acc[i][j][0], NORMAL | DENORMAL | ZERO);
+    again = __builtin_amdgcn_ballot_w64(again) != 0;
+    if (again) {
+        const Anew n;
+        again = false;
+#pragma unroll 1
+        for (int tile = 0; tile < TT * CT; ++tile) again |= any_beyond(n, t0 + 16 * (tile % TT), (c0 + 16 * (tile / TT)) / BLOCK);
+    }
+    if (again) {
+        const Anew n;
+#pragma unroll 1
+        for (int tile = 0; tile < TT * CT; ++tile) {
+            const int c = c0 + 16 * (tile / TT), t = t0 + 16 * (tile % TT) + (n.lane & 15), row = c + (n.lane & 15);
+            f32x4 v = tile_apart<EXACT>(n, t, row, c / BLOCK, wave + start, WAVES, mine, whole, f32x4{0, 0, 0, 0});
+            if (whole < a.blocks && wave == whole % WAVES) v = tile_apart<EXACT>(n, t, row, c / BLOCK, whole, 0, 1, INT32_MAX, v);
+            parts[wave][tile][n.lane] = v;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < CT; ++i)
+#pragma unroll
+            for (int j = 0; j < TT; ++j) parts[wave][i * TT + j][lane] = acc[i][j];
+    }
     __syncthreads();
     for (int e = tid; e < TT * CT * 64; e += 64 * WAVES) {
         const int tile = e >> 6, from = e & 63;
@@ -393,6 +498,7 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
 
     // ---- products ----
     f32x4 acc[TI][TJ];
+    float low = 1.0f;               // the least product of scales (0: sums that are not finite were met)
     // lane addresses of its operand rows (pieces g; pieces g + 4 lie 64 bytes on or back)
     const int xr = 16 * TJ * wt + l16, wr = 16 * TI * wc + tile_row<EXACT>(0, l16);
     const int xa = xr * BLOCK + 16 * (g ^ (l16 >> 1));
@@ -438,6 +544,7 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
             if (q < TI) w[i].set(wraw[i][0], wraw[i][1]);
             if (q < TI * TJ && i == 0) {
                 scale[j & 1] = f[j & 1] * wsb;
+                if (j & 1) low = fminf(fminf(low, fabsf(scale[0])), fabsf(scale[1]));
                 x.set(xraw[j & 1][0], xraw[j & 1][1]);
                 if (j + 1 < TJ) {
                     read_x(at, j + 1);
@@ -467,6 +574,8 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
     // A lane has runs of 8 (bf16) or 4 (fp32) neighbouring channels of TJ tokens.
     auto store = [&](const Place &tile) {
         const int c = tile.c0 + 16 * TI * wc;
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) low = is(acc[0][j][0], NORMAL | DENORMAL | ZERO) ? low : 0.0f;
         if (tile.c0 + T::CHANNELS <= a.n && tile.t0 + T::TOKENS <= a.tokens) {
             float bias[TI][4];
 #pragma unroll
@@ -516,6 +625,26 @@ __global__ __launch_bounds__(64 * WT * WC) void product_kernel(ProductArgs a, in
         copy();                     // ahead of the outputs, which the next blocks then need not wait for
         sent = true;
         store(tile);
+    }
+
+    if (!__builtin_amdgcn_ballot_w64(is(low, ANY - NORMAL))) return;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // (before outputs are written again)
+    const Anew n;
+    const int m = n.lane & 15;
+#pragma unroll 1
+    for (int mine = blockIdx.x; mine < total; mine += gridDim.x) {
+        const Place tile = place(mine);
+        const int c = tile.c0 + 16 * TI * wc;
+        bool again = false;
+#pragma unroll 1
+        for (int j = 0; j < TJ; ++j) again |= any_beyond(n, tile.t0 + 16 * (TJ * wt + j), c / BLOCK);
+        if (!again) continue;
+#pragma unroll 1
+        for (int ij = 0; ij < TI * TJ; ++ij) {
+            const int i = ij / TJ, t = tile.t0 + 16 * (TJ * wt + ij % TJ) + m;
+            const f32x4 v = tile_apart<EXACT>(n, t, c + tile_row<EXACT>(i, m), c / BLOCK, 0, 1, n.a.blocks, n.a.blocks, f32x4{0, 0, 0, 0});
+            store4(n.a, t, c + tile_row<EXACT>(i, 4 * (n.lane >> 4)), v);
+        }
     }
 }
 
