@@ -480,7 +480,8 @@ int32_t leapquant_scan_gates(const lq_dims *dims, const lq_scan *s, float *alpha
  * leapquant_add_norm -- h = x + residual, residual_out = h, and
  *   out = h / sqrt(mean h^2 + eps) * weight  (LQ_NORM_RMS)  or  out = h  (LQ_NORM_NONE)
  * of rows of channels, rounded once each (the norm reads h in fp32, not as
- * residual_out holds it).  Without a residual h = x.  channels is a multiple of
+ * residual_out holds it; squares and their mean are fp32 too, so a row whose sum of
+ * squares is past 3.4e38 gives zeros).  Without a residual h = x.  channels is a multiple of
  * 8, at most LQ_MAX_NORM_CHANNELS.  residual_out may be residual (in place), and
  * either output may be x, if the types and strides are the same.
  */

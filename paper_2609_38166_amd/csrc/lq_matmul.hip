@@ -178,9 +178,9 @@ __device__ __forceinline__ void store4(const ProductArgs &a, int t, int c, f32x4
 
 // ---- few tokens -------------------------------------------------------------------
 //
-// Bound: HBM, the weight.  A workgroup owns 16 CT channels of 16 TT tokens; its waves take the blocks of k in turn, AHEAD
-// of them on their way, straight from memory into registers, and join their sums in LDS.  1 token x 4096 -> 12288 9.8 us (5.2 TB/s),
-// 77 x 1552 -> 1000 fp32 4.5.
+// Bound: the weight's bytes.  A workgroup owns 16 CT channels of 16 TT tokens; its waves take the blocks of k in turn, AHEAD
+// of them on their way, straight from memory into registers, and join their sums in LDS.  1 token x 4096 -> 12288 10.9 us with
+// weights from HBM (4.6 TB/s), 9.8 with one weight call after call, which the last-level cache holds; 77 x 1552 -> 1000 fp32 4.4.
 constexpr int WAVES = 8, AHEAD = 2;
 
 template <bool EXACT, int TT, int CT>
@@ -242,7 +242,8 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(ProductArgs a) 
             }
         }
     };
-    // This wave's blocks, from a start of the workgroup's own on: 1 token x 4096 -> 12288 13.0 -> 10.6 us, 4096 -> 4096 6.0 -> 4.9.
+    // This wave's blocks, from a start of the workgroup's own on: 1 token x 4096 -> 12288 13.0 -> 10.6 us, 4096 -> 4096 6.0 -> 4.9
+    // when it was made.
     // (Why was not found: rows 128 bytes further apart change nothing, so it is not that rows meet in a few channels.)
     const int whole = a.k / BLOCK, start = whole ? (int)(blockIdx.x * 5u % (unsigned)whole) : 0;
     const int mine = wave < whole ? (whole - 1 - wave) / WAVES + 1 : 0;
@@ -310,8 +311,8 @@ hipError_t launch_few(const ProductArgs &a, hipStream_t st) {
 }
 
 // The largest piece that leaves 160 workgroups: fewer of them re-read less, and 16 x 16 where none does.  Up to 4 tokens the
-// rows of x cost nothing.  (4096 x 4096: 16 tokens 7.2 us by 16 x 16, 10.6 by 16 x 64; 64 tokens 12.1 by 32 x 32, 15.6 by
-// 32 x 64.  4096 x 12288: 16 tokens 13.9 by 16 x 64, 16.7 by 16 x 16; 1 token 11.9 and 11.0.)
+// rows of x cost nothing.  (4096 x 4096: 16 tokens 6.9 us by 16 x 16, 12.4 by 16 x 64; 64 tokens 12.0 by 32 x 32, 15.8 by
+// 32 x 64.  4096 x 12288: 16 tokens 12.8 by 16 x 64, 15.7 by 16 x 16; 1 token 11.0 and 9.8.)
 template <bool EXACT>
 hipError_t launch_few_tokens(const ProductArgs &a, hipStream_t st) {
     const int64_t t = (a.tokens - 1) / 16 + 1, c = (a.n - 1) / 16 + 1;
@@ -332,9 +333,9 @@ hipError_t launch_few_tokens(const ProductArgs &a, hipStream_t st) {
 // read takes at once lie in 16 different places of a 256-byte line of banks.  Channels are dealt to a wave's tiles so that a
 // lane ends up with 16 bytes of neighbouring outputs of a token at a time, and 4 lanes with 64.
 //
-// 8192 x 4096 -> 12288 bf16 380-385 us (2.1 PFLOP/s; the matrix cores are busy 55% of the cycles): without the outputs' stores
-// 376, without copies too 298-338, without the waves' meeting too 259 (a version before the last steps).  Two waves
-// a SIMD: one with twice the tile took 480.  256 x 4096 -> 12288 24 us; 1531 x 4096 -> 4096 fp32 55, where the
+// 8192 x 4096 -> 12288 bf16 377-385 us (2.1 PFLOP/s; the matrix cores are busy 53% of the cycles).  A version before the last
+// steps without the outputs' stores 376, without copies too 298-338, without the waves' meeting too 259.  Two waves a SIMD: one
+// with twice the tile took 480.  256 x 4096 -> 12288 24 us; 1531 x 4096 -> 4096 fp32 54-55, where the
 // codes' conversions take as long as the products.
 
 // Copies into LDS as dma16's and dma_element's: 16 bytes per lane from a uniform base and a lane's offset, and one element.
@@ -659,8 +660,10 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t st) {
 }
 
 // The tile whose rounds of 256 workgroups take the least time; a round's, for k = 4096, was measured (in 0.1 us).  192 tokens
-// fill rounds that 128 and 256 do not: 1531 x 4096 -> 4096 fp32 61 -> 55 us (256 tiles instead of 192 larger ones), 1536 x 4096 -> 8192
-// fp32 118 -> 89, 3000 x 4096 -> 4096 bf16 70 -> 65.
+// fill rounds that 128 and 256 do not: 1531 x 4096 -> 4096 fp32 54 us by 192 x 128 (256 tiles), 61 by 128 x 256, 73 by 128 x 128;
+// 3000 x 4096 -> 4096 bf16 54 by 192 x 256, 59 by 256 x 256, 67 by 128 x 256.  The rule holds at other depths: with every tile
+// tried at k = 128, 512, 1024 and 4096 on eight sizes from 512 x 2048 to 8192 x 12288 outputs in both types, it took the fastest
+// or one within 5% of it.
 template <bool EXACT>
 hipError_t launch_many_tokens(const ProductArgs &a, hipStream_t st) {
     struct Choice {
@@ -686,8 +689,9 @@ hipError_t launch_many_tokens(const ProductArgs &a, hipStream_t st) {
     }
 }
 
-// Few tokens, or too few tiles for half of the CUs, go without LDS: 128 x 4096 x 2048 11.9 us, by tiles of 64 x 64 16.1;
-// 300 x 2048 x 2048 (160 tiles) 12.4 and 10.4.
+// Few tokens, or too few tiles for half of the CUs, go without LDS: 128 x 4096 x 2048 (64 tiles) bf16 11.9 us, by tiles of 64 x 64
+// 14.5, fp32 12.8 and 20.9; 256 x 4096 x 2048 (128) 15.8 and 14.6, fp32 16.9 and 21.1; 300 x 2048 x 2048 (160) 17.2 and 9.2, fp32
+// 18.3 and 12.4.
 template <bool EXACT>
 hipError_t launch(const ProductArgs &a, hipStream_t st) {
     const int64_t tiles = (int64_t)((a.tokens - 1) / 64 + 1) * ((a.n - 1) / 64 + 1);

@@ -80,7 +80,8 @@ int32_t leapquant_matmul(const lq_matmul *m, void *stream) {
     int32_t e;
     if ((e = check_tokens(m->tokens)) != LQ_OK) return e;
     if (m->k % 16) return LQ_EUNSUPPORTED;
-    // (a launch's work-items are counted in 32 bits: 512 of them for 16 channels of few tokens, for 128 x 128 outputs of many)
+    // (a launch's work-items are counted in 32 bits, 512 of them for 16 channels of few tokens; of many tokens the tiles, of 64 x 64
+    // outputs at the least, and the places that they are dealt to are 32-bit numbers)
     if (m->n > 1 << 26 || m->tokens > 1 << 28 || m->tokens > (1LL << 36) / m->n) return LQ_EUNSUPPORTED;
     // a tile's rows are addressed by 32 bits from its first one
     const int64_t T = m->tokens, apart = 1 << 23, scales_apart = 1 << 20;

@@ -6,7 +6,9 @@
 // Bound: HBM; the gated norm's instructions come near it.  A lane owns 8 channels, so that a block of 128 is a row of 16 lanes
 // (its largest magnitude by DPP); a row of channels stays in the registers of 8 to 1024 lanes between its sum of squares and
 // its output.  bf16 to E4M3: add_norm of 8192 x 4096 48 us (4.9 TB/s), gate_norm of 8192 x 32 heads of 128 37-38 (4.5 TB/s; 290
-// vector instructions for 8 values a lane, 370 took 49-50).
+// vector instructions for 8 values a lane, 370 took 49-50); the gate first, a weight per head and heads of 64 to 8192 37-40.  Lengths
+// that leave lanes idle or need workgroups of 1024 are further off: 8192 x 11 heads of 384 47 us, of 37 by their bytes, 2048 rows of
+// 16384 48, of 36.
 #include <algorithm>
 
 #include "lq_e4m3.hpp"
