@@ -6,10 +6,11 @@ import subprocess
 
 import pytest
 
+from paper_2609_38166_amd import build
 from tests import projection_sizes as Z
-from tests.test_sanitizers import CLANG, HIPCC, ROOT, _run
 
-CSRC = os.path.join(ROOT, "paper_2609_38166_amd", "csrc")
+CSRC = os.path.join(build.PKG, "csrc")
+CLANG = "/opt/rocm/llvm/bin/clang++"
 
 
 def kernel(name):
@@ -22,17 +23,17 @@ def kernel(name):
 
 @pytest.fixture(scope="module")
 def choose(tmp_path_factory):
-    if not (os.path.exists(HIPCC) and os.path.exists(CLANG)):
+    if not (os.path.exists(build.HIPCC) and os.path.exists(CLANG)):
         pytest.skip("hipcc / clang++ not found")
     path = tmp_path_factory.mktemp("choice")
     objs = []
-    for src in (os.path.join(CSRC, "lq_matmul.hip"), os.path.join(ROOT, "tests", "host", "product_choice.cpp")):
+    for src in (os.path.join(CSRC, "lq_matmul.hip"), os.path.join(build.ROOT, "tests", "host", "product_choice.cpp")):
         objs.append(str(path / (os.path.basename(src) + ".o")))
-        _run([HIPCC, "-x", "hip", "-std=c++17", "-O1", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "--offload-host-only", "-c", src,
-              "-o", objs[-1]], str(path))
+        subprocess.run([build.HIPCC, "-x", "hip", "-std=c++17", "-O1", "-I", os.path.join(build.ROOT, "include"), "-I", CSRC,
+                        "--offload-host-only", "-c", src, "-o", objs[-1]], check=True)
     exe = str(path / "product_choice")
     # (the device code that is not there is never looked at)
-    _run([CLANG, *objs, "-no-pie", "-Wl,--unresolved-symbols=ignore-all", "-o", exe], str(path))
+    subprocess.run([CLANG, *objs, "-no-pie", "-Wl,--unresolved-symbols=ignore-all", "-o", exe], check=True)
 
     def run(sizes):
         """All kernels, and of each (tokens, k, n, type): its kernel, workgroups and tiles."""
