@@ -50,7 +50,7 @@ def product(x, xs, w, ws, out):
     return y
 
 
-@pytest.mark.parametrize("case", Z.one_each(), ids=Z.name)
+@pytest.mark.parametrize("case", Z.one_each() + Z.several(), ids=Z.name)
 def test_scales_whose_product_is_no_normal_number(case):
     _, tokens, n, out = case
     (x, xs), (w, ws) = rows(tokens), weight(n)
@@ -67,7 +67,7 @@ def test_scales_whose_product_is_no_normal_number(case):
     assert (y[4::CLASSES] == 0).all()
 
 
-@pytest.mark.parametrize("case", Z.one_each(), ids=Z.name)
+@pytest.mark.parametrize("case", Z.one_each() + Z.several(), ids=Z.name)
 def test_ordinary_rows_keep_their_bits_beside_such_scales(case):
     _, tokens, n, out = case
     (x, xs), (w, ws) = rows(tokens), weight(n)
@@ -101,3 +101,25 @@ def test_encoded_rows_of_the_least_scales():
         want, mag = R.matmul(x8, xs, w8, ws)
         assert ((y.double().cpu() - want).abs() <= 300 * U * mag + 5 * 2.0 ** -150).all()
         assert (y[3] == 0).all() and float(want.abs().max()) > least
+
+
+@pytest.mark.parametrize("tokens,n", [(16, 272), (320, 1664), (8256, 1408)])
+def test_a_captured_call_follows_its_scales(tokens, n):
+    """Replays with ordinary scales, with such scales and with ordinary ones again, eager calls in between."""
+    (x, xs), (w, ws) = rows(tokens), weight(n)
+    x, w, plain, plain_w = x.cuda(), w.cuda(), scales(21, tokens, BLOCKS).cuda(), scales(22, R.blocks(n), BLOCKS).cuda()
+    turns = [(plain, plain_w), (xs.cuda(), ws.cuda()), (plain, plain_w), (xs.cuda(), plain_w)]
+    want = [product(x, a, w, b, torch.float32) for a, b in turns]
+    sx, sw, y = plain.clone(), plain_w.clone(), torch.empty((tokens, n), device="cuda")
+    B.leapquant_matmul(x, sx, w, sw, y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.leapquant_matmul(x, sx, w, sw, y)
+    for (a, b), expected in zip(turns, want):
+        sx.copy_(a)
+        sw.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, expected)
+        assert torch.equal(product(x, a, w, b, torch.float32), expected)
